@@ -518,6 +518,61 @@ size_t sdrop_bias_grad_workspace_bytes(int64_t M, int64_t K, int BM, int BK);
 int sdrop_bias_grad(const void *dZ, const void *mask, float *db, int64_t M, int64_t K, int BM, int BK,
                     int dtype, int64_t ld_dz, void *ws, size_t ws_bytes, void *stream);
 
+/*
+ * ---- Around the substituted layers: what else a transformer block is made of (Section 4.2's ViT and GPT) ----
+ *
+ * These entry points have sizes of any value: no column count has to be a multiple of anything, leading dimensions are 0
+ * (contiguous) or at least the number of columns and at most 2^24, pointers need the alignment of one element.  M <= 2^30,
+ * N <= 2^24.  `dtype` is SDROP_F16, SDROP_BF16 or SDROP_F32, of all matrices of a call.  Everything is computed in fp32 and
+ * rounded to nearest even where it is written.
+ *
+ * Element dropout (the paper's baseline, Section 2.1), with a mask that is never stored:
+ *
+ *     Y = R + m X / (1 - p')                R may be NULL (no residual)
+ *
+ * m[i][j] is a function of (seed, rng_stream, i, j, N, p) alone, so the backward pass is the same call on dY without R.  One
+ * Philox4x32-10 call with counter (c lo32, c hi32 | 2^31, rng_stream lo32, rng_stream hi32) and key (seed lo32, seed hi32) serves
+ * the 8 elements j = 8 b .. 8 b + 7 of row i, c = i * ceil(N / 8) + b: element j has the 16 bits number j % 8 of the four output
+ * words (low half first) and is kept where they are >= t = round(65536 p) (at most 65535 for p < 1).  p' = t / 65536, so that
+ * the expected value is exact; p = 1 drops everything.  A dropped element of X counts as 0 whatever it holds.
+ * Y may be X or R (with the same leading dimension).
+ */
+int sdrop_dropout(const void *X, const void *R, void *Y, int64_t M, int64_t N, double p, uint64_t seed, uint64_t rng_stream,
+                  int dtype, int64_t ld_x, int64_t ld_r, int64_t ld_y, void *stream);
+
+/*
+ * Layer norm over the N columns of each row, with the dropout and the residual add in front of it where the call has them:
+ *
+ *     H = R + m X / (1 - p')   rounded to `dtype` (the residual stream; as sdrop_dropout)
+ *     Y = (H - mean) rstd gamma + beta,   rstd = 1 / sqrt(var + eps), var = mean of (H - mean)^2
+ *
+ *   R       may be NULL (nothing added).  H: NULL only where R is NULL and p = 0 (H is X itself); it may be X or R.
+ *   gamma, beta   N values of type `w_dtype` (`dtype` or SDROP_F32); beta may be NULL (0)
+ *   mean, rstd    fp32[M], for the backward pass; either may be NULL
+ *   Y       may be X where H is NULL
+ */
+int sdrop_layer_norm(const void *X, const void *R, const void *gamma, const void *beta, void *H, void *Y, float *mean, float *rstd,
+                     int64_t M, int64_t N, double eps, double p, uint64_t seed, uint64_t rng_stream, int dtype, int w_dtype,
+                     int64_t ld_x, int64_t ld_r, int64_t ld_h, int64_t ld_y, void *stream);
+
+/*
+ * Its backward pass.  With z = (H - mean) rstd and w = dY gamma:
+ *
+ *     dR = dH + rstd (w - mean(w) - z mean(w z))     dH: the gradient that reaches H from elsewhere, NULL: none
+ *     dX = m dR / (1 - p')                           m as in the forward call with the same p, seed and rng_stream
+ *     dgamma = sum over rows of dY z, dbeta = sum over rows of dY
+ *
+ *   dR, dX, dgamma, dbeta   any may be NULL, not all.  With p = 0, dX = dR.  dgamma and dbeta have type `w_dtype`.
+ *                           dR may be dY or dH, dX may be dY (with the same leading dimension).
+ *   ws, ws_bytes            sdrop_layer_norm_bwd_workspace_bytes(M, N) bytes, 16-byte aligned, where dgamma or dbeta is wanted: fp32
+ *                           rows that a second launch adds in a fixed order (the result does not depend on scheduling)
+ */
+size_t sdrop_layer_norm_bwd_workspace_bytes(int64_t M, int64_t N);
+int sdrop_layer_norm_bwd(const void *dY, const void *dH, const void *H, const void *gamma, const float *mean, const float *rstd,
+                         void *dR, void *dX, void *dgamma, void *dbeta, int64_t M, int64_t N, double p, uint64_t seed,
+                         uint64_t rng_stream, int dtype, int w_dtype, int64_t ld_dy, int64_t ld_dh, int64_t ld_h, int64_t ld_dr,
+                         int64_t ld_dx, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,7 +27,8 @@ EXPORTS = ("sdrop_strerror", "sdrop_last_hip_error", "sdrop_status", "sdrop_set_
            "sdrop_fwd", "sdrop_fwd_seeded", "sdrop_fwd_seeded_ex", "sdrop_fwd_seeded_bias", "sdrop_fwd_dense", "sdrop_bwd_dx", "sdrop_bwd_dw", "sdrop_bwd_dw_static",
            "sdrop_bwd", "sdrop_bwd_ex", "sdrop_fwd_ex", "sdrop_bwd_dx_ex", "sdrop_bwd_dw_ex", "sdrop_workspace_bytes_ex",
            "sdrop_producer", "sdrop_producer_ex", "sdrop_producer_zeroed", "sdrop_bwd_gated", "sdrop_producer_bwd",
-           "sdrop_bias_grad_workspace_bytes", "sdrop_bias_grad", "sdrop_col_sum_workspace_bytes", "sdrop_col_sum")
+           "sdrop_bias_grad_workspace_bytes", "sdrop_bias_grad", "sdrop_col_sum_workspace_bytes", "sdrop_col_sum",
+           "sdrop_dropout", "sdrop_layer_norm", "sdrop_layer_norm_bwd_workspace_bytes", "sdrop_layer_norm_bwd")
 
 SCALE_DROPOUT, SCALE_ONE = 0, 1
 ACT_NONE, ACT_RELU, ACT_GELU_TANH, ACT_GELU_ERF = 0, 1, 2, 3
@@ -137,6 +138,14 @@ def lib():
         L.sdrop_col_sum_workspace_bytes.restype = sz
         L.sdrop_col_sum.argtypes = [vp, vp, i64, i64, ci, i64, vp, sz, vp]
         L.sdrop_col_sum.restype = ci
+        L.sdrop_dropout.argtypes = [vp, vp, vp, i64, i64, dbl, u64, u64, ci, i64, i64, i64, vp]
+        L.sdrop_dropout.restype = ci
+        L.sdrop_layer_norm.argtypes = [vp] * 8 + [i64, i64, dbl, dbl, u64, u64, ci, ci, i64, i64, i64, i64, vp]
+        L.sdrop_layer_norm.restype = ci
+        L.sdrop_layer_norm_bwd_workspace_bytes.argtypes = [i64, i64]
+        L.sdrop_layer_norm_bwd_workspace_bytes.restype = sz
+        L.sdrop_layer_norm_bwd.argtypes = [vp] * 10 + [i64, i64, dbl, u64, u64, ci, ci, i64, i64, i64, i64, i64, vp, sz, vp]
+        L.sdrop_layer_norm_bwd.restype = ci
         _lib = L
     return _lib
 
@@ -732,3 +741,103 @@ def sdrop_col_sum(dY, out=None, ws=None):
                              ws.numel() * ws.element_size(), _stream())
     _check(rc, "sdrop_col_sum")
     return out
+
+
+# ---- around the substituted layers: element dropout, layer norm ----
+
+def _on_current_device(t):
+    """Launches go to the current device's stream: a tensor of another device is refused here (its kernels would fault there)."""
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current device: call under torch.cuda.device(%d)" % t.device.index)
+
+
+def _row_types(name, x, *others):
+    """The common type of a row operator's matrices."""
+    if x.dtype not in _DTYPES:
+        raise SdropError(EDTYPE, name)
+    if any(t is not None and t.dtype != x.dtype for t in others):
+        raise ValueError("%s: matrices must have the same dtype" % name)
+    return _DTYPES[x.dtype]
+
+
+def _opt_mat(t, name, shape):
+    """_mat of a matrix that may be missing: (None, 0) then."""
+    if t is None:
+        return None, 0
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has the wrong shape" % name)
+    return _mat(t, name)
+
+
+def _weight(t, name, n, dtype):
+    """Address of a norm's weight: n values of the matrices' type or fp32."""
+    if t is None:
+        return None
+    if tuple(t.shape) != (n,) or t.dtype not in (dtype, torch.float32):
+        raise ValueError("%s must have one value per column, of the matrices' dtype or fp32" % name)
+    return _dev(t, name)
+
+
+def sdrop_dropout(X, p, seed, rng_stream=0, residual=None, out=None):
+    """Y = residual + m . X / (1 - p): element dropout whose mask is drawn where it is needed and never stored (see the header for
+    the generator).  The backward pass is the same call on dY without the residual.  X [M, N] fp16 / bf16 / fp32 with
+    contiguous rows (a leading dimension is allowed)."""
+    M, N = X.shape
+    dt = _row_types("sdrop_dropout", X, residual, out)
+    if out is None:
+        out = torch.empty((M, N), dtype=X.dtype, device=X.device)
+    (px, ldx), (pr, ldr), (po, ldo) = _mat(X, "X"), _opt_mat(residual, "residual", (M, N)), _opt_mat(out, "out", (M, N))
+    _on_current_device(X)
+    _check(lib().sdrop_dropout(px, pr, po, M, N, float(p), int(seed), int(rng_stream), dt, ldx, ldr, ldo, _stream()), "sdrop_dropout")
+    return out
+
+
+def sdrop_layer_norm(X, gamma, beta=None, eps=1e-5, residual=None, p=0.0, seed=0, rng_stream=0, out=None, out_h=None):
+    """Layer norm of the rows of H = residual + m . X / (1 - p) (of X itself without a residual and with p = 0).
+    Returns (Y, H, mean, rstd); H is X where nothing is added or dropped, else the residual stream's new tensor.
+    X [M, N] fp16 / bf16 / fp32 with contiguous rows; gamma and beta (or None) have X's type or fp32."""
+    M, N = X.shape
+    dt = _row_types("sdrop_layer_norm", X, residual, out, out_h)
+    if beta is not None and beta.dtype != gamma.dtype:
+        raise ValueError("gamma and beta must have the same dtype")
+    fused = residual is not None or p != 0.0
+    if out is None:
+        out = torch.empty((M, N), dtype=X.dtype, device=X.device)
+    if out_h is None and fused:
+        out_h = torch.empty((M, N), dtype=X.dtype, device=X.device)
+    stats = torch.empty((2, M), dtype=torch.float32, device=X.device)
+    (px, ldx), (pr, ldr) = _mat(X, "X"), _opt_mat(residual, "residual", (M, N))
+    (ph, ldh), (py, ldy) = _opt_mat(out_h, "out_h", (M, N)), _opt_mat(out, "out", (M, N))
+    pg, pb = _weight(gamma, "gamma", N, X.dtype), _weight(beta, "beta", N, X.dtype)
+    _on_current_device(X)
+    at = stats.data_ptr()
+    _check(lib().sdrop_layer_norm(px, pr, pg, pb, ph, py, at, at + 4 * M, M, N, float(eps), float(p), int(seed), int(rng_stream),
+                                  dt, _DTYPES[gamma.dtype], ldx, ldr, ldh, ldy, _stream()), "sdrop_layer_norm")
+    return out, X if out_h is None else out_h, stats[0], stats[1]
+
+
+def sdrop_layer_norm_bwd(dY, H, gamma, mean, rstd, dH=None, p=0.0, seed=0, rng_stream=0, need_dr=True, need_dx=True,
+                         need_dgamma=True, need_dbeta=True, ws=None):
+    """The gradients of sdrop_layer_norm: returns (dX, dR, dgamma, dbeta).  dH: the gradient that reaches H from elsewhere.
+    With p = 0, dX is dR.  What is not needed is None; p, seed and rng_stream are those of the forward call."""
+    M, N = dY.shape
+    dt = _row_types("sdrop_layer_norm_bwd", dY, H, dH)
+    for s, name in ((mean, "mean"), (rstd, "rstd")):
+        if s.dtype != torch.float32 or tuple(s.shape) != (M,):
+            raise ValueError("%s must be fp32 with one value per row" % name)
+    drops = p != 0.0
+    dr = torch.empty((M, N), dtype=dY.dtype, device=dY.device) if need_dr or (need_dx and not drops) else None
+    dx = torch.empty((M, N), dtype=dY.dtype, device=dY.device) if need_dx and drops else None
+    dg = torch.empty_like(gamma) if need_dgamma else None
+    db = torch.empty_like(gamma) if need_dbeta else None
+    if dr is None and dx is None and dg is None and db is None:
+        return None, None, None, None
+    if ws is None and (need_dgamma or need_dbeta):
+        ws = torch.empty(max(int(lib().sdrop_layer_norm_bwd_workspace_bytes(M, N)), 16), dtype=torch.uint8, device=dY.device)
+    (py, ldy), (pdh, lddh), (ph, ldh) = _mat(dY, "dY"), _opt_mat(dH, "dH", (M, N)), _opt_mat(H, "H", (M, N))
+    pg, at = _weight(gamma, "gamma", N, dY.dtype), [None if t is None else t.data_ptr() for t in (dr, dx, dg, db)]
+    _on_current_device(dY)
+    _check(lib().sdrop_layer_norm_bwd(py, pdh, ph, pg, _dev(mean, "mean"), _dev(rstd, "rstd"), *at, M, N, float(p), int(seed), int(rng_stream),
+                                      dt, _DTYPES[gamma.dtype], ldy, lddh, ldh, 0, 0, None if ws is None else ws.data_ptr(),
+                                      0 if ws is None else ws.numel() * ws.element_size(), _stream()), "sdrop_layer_norm_bwd")
+    return (dx if drops else dr if need_dx else None), (dr if need_dr else None), dg, db
