@@ -93,6 +93,7 @@ int sdrop_set_tuning(int knob, int value);
  * pointer.
  */
 #define SDROP_STATUS_MASK_MISMATCH 1
+#define SDROP_STATUS_BAD_LENGTHS 2      /* attention: offsets or lengths of a sequence that do not fit the call */
 int sdrop_status(int *flags_host, int clear, void *stream);
 
 /* Text for an error code (static storage). */
@@ -572,6 +573,65 @@ int sdrop_layer_norm_bwd(const void *dY, const void *dH, const void *H, const vo
                          void *dR, void *dX, void *dgamma, void *dbeta, int64_t M, int64_t N, double p, uint64_t seed,
                          uint64_t rng_stream, int dtype, int w_dtype, int64_t ld_dy, int64_t ld_dh, int64_t ld_h, int64_t ld_dr,
                          int64_t ld_dx, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Attention.  For each sequence, query head and query token i:
+ *
+ *     S[j] = scale q_i . k_j,   P = softmax of S over the keys j that token i sees,   O_i = sum over j of P[j] v_j
+ *     lse_i = log of the sum over those j of exp(S[j])
+ *
+ * Query head h reads key / value head h / (Hq / Hkv).  Token i of Lq sees all Lk keys of its sequence or, causal, the keys
+ * j <= i + Lk - Lq (the last token sees every key: new tokens behind a cache).  A token that sees no key has O = 0, lse = -inf.
+ * Products run on the matrix cores; scores, statistics and sums are fp32, P is rounded to `dtype` for the second product.  A key
+ * that a token does not see has P = 0 whatever its score; its v still takes part as 0 times v (as in the formula), so it has to
+ * be finite, except behind k_len and between packed sequences, where nothing is read.
+ *
+ *   q, k, v, o     element (sequence b, token t, head h, d) lies at b * x_b + t * x_t + h * x_h + d: strides in elements, multiples of
+ *                  8 (token strides at most 2^24; stride 0 repeats an input); pointers are 16-byte aligned.  [tokens, heads, D]
+ *                  and [heads, tokens, D], slices of a fused projection and of a wider cache are all taken in place.
+ *   B, max_q, max_k   dense: B sequences of max_q queries and max_k keys
+ *   cu_q, cu_k     NULL, or device int32[B+1]: packed sequences; sequence b has rows cu[b] .. cu[b+1] - 1 of the total_q (total_k) rows of
+ *                  the array, the *_b strides are not used, and max_q (max_k) is an upper bound of the lengths, of which any may be 0.
+ *                  Rows behind the last sequence are left as they were.
+ *   k_len          NULL, or (without cu_k) device int32[B]: sequence b has k_len[b] <= max_k keys; what lies behind them is not read
+ *   D              head size: a multiple of 8, at most 128
+ *   lse            NULL, or fp32: [B, Hq, max_q], packed [Hq, total_q]
+ *   o_rest         NULL, or an array like o (its strides, its alignment) that receives what o's rounding took, rounded in turn:
+ *                  the backward pass needs row sums of dO O, whose error would otherwise be that of a rounded O
+ *   ws, ws_bytes   sdrop_attn_workspace_bytes(a) bytes (partial results where few queries share many keys out to the whole
+ *                  chip; may be 0), 16-byte aligned
+ *
+ * Offsets and lengths are device data: a sequence whose values do not fit the call (descending, beyond the array, longer than the
+ * bound) is left out, nothing of it is read or written, and SDROP_STATUS_BAD_LENGTHS is set (see sdrop_status).
+ */
+typedef struct sdrop_attn {
+    int64_t B, max_q, max_k, Hq, Hkv, D;
+    int64_t total_q, total_k;
+    const int32_t *cu_q, *cu_k, *k_len;
+    int64_t q_b, q_t, q_h, k_b, k_t, k_h, v_b, v_t, v_h, o_b, o_t, o_h;
+    int64_t do_b, do_t, do_h, dq_b, dq_t, dq_h, dk_b, dk_t, dk_h, dv_b, dv_t, dv_h;     /* sdrop_attn_bwd only */
+    double scale;
+    int32_t causal, dtype;
+} sdrop_attn_t;
+
+size_t sdrop_attn_workspace_bytes(const sdrop_attn_t *a);
+int sdrop_attn(const void *q, const void *k, const void *v, void *o, void *o_rest, float *lse, const sdrop_attn_t *a, void *ws,
+               size_t ws_bytes, void *stream);
+
+/*
+ * Its backward pass, from o, o_rest (or NULL) and lse of the forward call with the same description:
+ *
+ *     P = exp(S - lse), dP = dO v^T, dS = P (dP - row sums of dO o):   dq = scale dS k,  dk = scale dS^T q,  dv = P^T dO
+ *
+ * P and dS are rounded to `dtype` for their products, sums are fp32, dk and dv summed over the query heads that share them.  The
+ * order of all sums is fixed: results repeat bit for bit.  dq, dk and dv are written completely (dk and dv are 0 behind k_len;
+ * rows behind the last packed sequence are left as they were) and may be slices of one buffer; none may overlap an input.
+ * Strides must not be 0 in an output.
+ *   ws, ws_bytes   sdrop_attn_bwd_workspace_bytes(a) bytes, 16-byte aligned
+ */
+size_t sdrop_attn_bwd_workspace_bytes(const sdrop_attn_t *a);
+int sdrop_attn_bwd(const void *dO, const void *q, const void *k, const void *v, const void *o, const void *o_rest, const float *lse,
+                   void *dq, void *dk, void *dv, const sdrop_attn_t *a, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -55,3 +55,42 @@ def layer_norm_bwd(dy, h, gamma, eps, dh=None):
     z, w = (h - mean[:, None]) * rstd[:, None], dy * gamma
     dr = rstd[:, None] * (w - w.mean(axis=1, keepdims=True) - z * (w * z).mean(axis=1, keepdims=True))
     return dr if dh is None else dr + dh, (dy * z).sum(axis=0), dy.sum(axis=0)
+
+
+def _scores(q, k, scale, causal):
+    s = scale * (q @ k.T)
+    if causal:
+        i, j = np.arange(q.shape[0])[:, None], np.arange(k.shape[0])[None, :]
+        s = np.where(j <= i + k.shape[0] - q.shape[0], s, -np.inf)
+    top = s.max(axis=1, initial=-np.inf)
+    ref = np.where(np.isfinite(top), top, 0.0)[:, None]
+    e = np.exp(s - ref)
+    total = e.sum(axis=1, keepdims=True)
+    with np.errstate(divide="ignore"):
+        lse = np.log(total[:, 0]) + ref[:, 0]
+    return e / np.where(total > 0, total, 1.0), lse
+
+
+def attention(q, k, v, scale, causal):
+    """One sequence: q [Tq, Hq, D], k and v [Tk, Hkv, D] -> (o, lse [Hq, Tq]).  A token that sees no key has o = 0, lse = -inf."""
+    group = q.shape[1] // k.shape[1]
+    o, lse = np.zeros(q.shape), np.zeros((q.shape[1], q.shape[0]))
+    for h in range(q.shape[1]):
+        p, lse[h] = _scores(q[:, h], k[:, h // group], scale, causal)
+        o[:, h] = p @ v[:, h // group]
+    return o, lse
+
+
+def attention_bwd(do, q, k, v, scale, causal):
+    """(dq, dk, dv) of that sequence."""
+    group = q.shape[1] // k.shape[1]
+    dq, dk, dv = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)
+    for h in range(q.shape[1]):
+        j = h // group
+        p, _ = _scores(q[:, h], k[:, j], scale, causal)
+        dp = do[:, h] @ v[:, j].T
+        ds = p * (dp - (p * dp).sum(axis=1, keepdims=True))
+        dq[:, h] = scale * (ds @ k[:, j])
+        dk[:, j] += scale * (ds.T @ q[:, h])
+        dv[:, j] += p.T @ do[:, h]
+    return dq, dk, dv

@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libsdrop.so")
 # The longest units come first.
 UNITS = [("sdrop_gemm_inst.hip", "sdrop_gemm_%s_%d.o" % (t.lower(), part), ["-DSDROP_T=" + t, "-DSDROP_PART=%d" % part])
          for part in (1, 0, 3, 2, 5, 4) for t in ("F16", "BF16")]
-UNITS += [(src, os.path.splitext(src)[0] + ".o", []) for src in ("sdrop_rows.hip", "sdrop_gemm.hip", "sdrop_mask.hip", "sdrop_bias_grad.hip")]
+UNITS += [(src, os.path.splitext(src)[0] + ".o", []) for src in ("sdrop_rows.hip", "sdrop_attn_fwd.hip", "sdrop_attn_bwd.hip", "sdrop_gemm.hip", "sdrop_mask.hip", "sdrop_bias_grad.hip")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

@@ -1,0 +1,248 @@
+// What the attention kernels share: the problem's description, sequences and their bounds, tiles of keys or queries in LDS.
+//
+//     S = c Q K^T,  P = softmax over the keys a query may see,  O = P V
+//
+// Queries of the heads that share a key / value head are rows of one problem: row r of (sequence, key head) is token r / G,
+// head r % G of the group of G.  A tile of rows then reads each key once for the whole group.
+#ifndef SDROP_ATTN_COMMON_H
+#define SDROP_ATTN_COMMON_H
+#include "gemm_device_common.h"
+
+namespace sdrop {
+
+struct AttnParams {
+    const char *q, *k, *v, *o, *dout;       // o, dout: backward
+    const char *rest;                       // backward: what o's rounding took, or null
+    char *out, *out_rest, *dq, *dk, *dv;    // out_rest may be null
+    float *lse, *delta;
+    float *part_o, *part_lse;               // forward over parts of the keys: [splits][B * Hkv][max_rows][D] and [..] of them
+    // bytes between sequences (dense), tokens and heads
+    int64_t q_b, q_t, q_h, k_b, k_t, k_h, v_b, v_t, v_h, o_b, o_t, o_h, do_b, do_t, do_h;
+    int64_t dq_b, dq_t, dq_h, dk_b, dk_t, dk_h, dv_b, dv_t, dv_h;
+    const int32_t *cu_q, *cu_k, *k_len;
+    int64_t total_q, total_k;
+    int32_t B, max_q, max_k, Hq, Hkv, G, D, causal;
+    int32_t max_rows;                       // max_q * G
+    int32_t tiles, splits;                  // row tiles of the longest sequence; parts of the keys
+    uint32_t g_mul;                         // r / G = (mulhi(r, g_mul) + r) >> g_shift
+    int32_t g_shift;
+    float scale, c;                         // c = scale * log2(e)
+    int *status;
+};
+
+namespace {
+
+// One sequence of the call: where its tokens begin (rows of a packed array; 0 in dense ones) and how many there are.
+struct Sequence {
+    int64_t q0, k0;
+    int Lq, Lk;
+    bool ok;
+};
+
+// Lengths and offsets are device data: what does not fit the call is left out (nothing of that sequence is read or written) and
+// recorded in the status word.
+__device__ __forceinline__ Sequence sequence_of(const AttnParams &P, int b)
+{
+    Sequence s;
+    s.q0 = s.k0 = 0;
+    s.Lq = P.max_q;
+    s.Lk = P.max_k;
+    s.ok = true;
+    if (P.cu_q) {
+        const int a = uni(P.cu_q[b]), e = uni(P.cu_q[b + 1]);
+        s.q0 = a;
+        s.Lq = e - a;
+        s.ok = a >= 0 && e >= a && e <= P.total_q && s.Lq <= P.max_q;
+    }
+    if (P.cu_k) {
+        const int a = uni(P.cu_k[b]), e = uni(P.cu_k[b + 1]);
+        s.k0 = a;
+        s.Lk = e - a;
+        s.ok = s.ok && a >= 0 && e >= a && e <= P.total_k && s.Lk <= P.max_k;
+    } else if (P.k_len) {
+        s.Lk = uni(P.k_len[b]);
+        s.ok = s.ok && s.Lk >= 0 && s.Lk <= P.max_k;
+    }
+    if (!s.ok && P.status && threadIdx.x == 0) atomicOr(P.status, SDROP_STATUS_BAD_LENGTHS);
+    return s;
+}
+
+__device__ __forceinline__ int token_of(const AttnParams &P, int r)
+{
+    return (int)((__umulhi((uint32_t)r, P.g_mul) + (uint32_t)r) >> P.g_shift);
+}
+
+// Workgroup id -> (sequence and key head, unit).  Consecutive workgroups go to the eight XCDs in turn: eight heads at a time, one
+// for each XCD, so that the workgroups that read the same keys share an L2.
+__device__ __forceinline__ void place(const AttnParams &P, int units, int &bh, int &unit)
+{
+    const int n = P.B * P.Hkv, id = blockIdx.x;
+    const int g = id / (8 * units), rem = id - g * 8 * units;
+    const int here = n - 8 * g < 8 ? n - 8 * g : 8;
+    bh = uni(8 * g + rem % here);
+    unit = uni(rem / here);
+}
+
+// ---- tiles in LDS: [rows][HD] of 16-bit values, as they lie in memory ----
+//
+// 16-byte chunk c of row r lies in slot c ^ swz_a(r).  Operands are read along the rows (ds_read_b128: 16 consecutive rows, one
+// chunk) and across them (ds_read_b64_tr_b16: 4 consecutive rows x 64 bytes); the value puts the former on all banks and the
+// rows of the latter 64 bytes apart.  It is the same for every 16 rows.
+template <int HD> __device__ __forceinline__ int swz_a(int r)
+{
+    return HD >= 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+
+// Loads a tile of ROWS rows with NW wavefronts, HBM -> LDS without registers: one instruction fills 1 KiB, lane l its bytes
+// 16 l ..; the lane fetches the chunk whose slot that is.
+template <int HD, int ROWS, int NW> struct TileLoad {
+    static constexpr int ROW_BYTES = 2 * HD, RPI = 1024 / ROW_BYTES, PASSES = ROWS / (RPI * NW);
+    static_assert(ROWS % (RPI * NW) == 0 && (RPI * NW) % 16 == 0, "every pass covers the same rows of the swizzle");
+    uint32_t voff;
+    int row, chunk, wave;
+    __device__ __forceinline__ void init(int64_t stride, int w)
+    {
+        const int lane = threadIdx.x & 63;
+        wave = w;
+        row = RPI * w + (lane * 16) / ROW_BYTES;
+        chunk = ((lane * 16) % ROW_BYTES >> 4) ^ swz_a<HD>(row);
+        voff = (uint32_t)row * (uint32_t)stride + (chunk << 4);
+    }
+    // rows: how many of the tile exist; nch: 16-byte chunks of a row that do.  What does not is 0 in LDS.
+    __device__ __forceinline__ void issue(const char *base, int64_t stride, char *lds, int rows, int nch) const
+    {
+        if (rows >= ROWS && nch == HD / 8) {
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i, base += RPI * NW * stride) dma16(base, voff, lds + (wave + NW * i) * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i, base += RPI * NW * stride) {
+                char *const dst = lds + (wave + NW * i) * 1024;
+                if (row + RPI * NW * i < rows && chunk < nch) dma16(base, voff, dst);
+                else *reinterpret_cast<uint4 *>(dst + (threadIdx.x & 63) * 16) = make_uint4(0, 0, 0, 0);
+            }
+        }
+    }
+};
+
+// The same for a lane's own 64-bit address (see dma16).
+__device__ __forceinline__ void dma16_at(const char *src, const char *lds)
+{
+    const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)lds;
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(lds_base));
+}
+
+// What this wavefront has requested has landed, and so has everyone else's; nothing is moved across.
+__device__ __forceinline__ void landed()
+{
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Operand of 32 rows of a tile, reduction along them (16 columns from 16 kk): lane l has row base + l % 32, columns 16 kk + 8 (l / 32) ..
+template <int HD, class T> struct RowOperand {
+    const char *at;
+    int f;
+    __device__ __forceinline__ RowOperand(const char *lds)
+    {
+        const int l = threadIdx.x & 63;
+        at = lds + (l & 31) * (2 * HD);
+        f = (swz_a<HD>(l & 31) ^ (l >> 5)) << 4;
+    }
+    __device__ __forceinline__ typename In<T>::vec get(int base, int kk) const
+    {
+        return *reinterpret_cast<const typename In<T>::vec *>(at + (f ^ (kk << 5)) + base * (2 * HD));
+    }
+};
+
+// Operand of 32 columns of a tile, reduction across its rows (16 rows from 16 ks).  Lane l has column base + l % 32; its eight values
+// are rows 16 ks + 4 (l / 32) + {0 .. 3, 8 .. 11}: the order in which a 32 x 32 result lies in a lane's registers, so that such a
+// result is the other operand as it is.
+template <int HD, class T> struct ColOperand {
+    const char *lo;
+    int fl, fh;
+    __device__ __forceinline__ ColOperand(const char *lds)
+    {
+        const int l = threadIdx.x & 63, r = 4 * (l >> 5) + ((l & 15) >> 2), chunk = 2 * ((l >> 4) & 1) + ((l & 3) >> 1);
+        lo = lds + r * (2 * HD) + ((l & 1) << 3);
+        fl = (chunk ^ swz_a<HD>(r)) << 4;
+        fh = (chunk ^ swz_a<HD>(r + 8)) << 4;
+    }
+    __device__ __forceinline__ typename In<T>::vec get(int db, int ks) const
+    {
+        const char *const p = lo + ks * 16 * (2 * HD);
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + (fl ^ (db << 6))));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 8 * (2 * HD) + (fh ^ (db << 6))));
+        return __builtin_bit_cast(typename In<T>::vec, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// Eight values of a 32 x 32 result (registers 8 part .. 8 part + 7) rounded to the operands' type.
+template <class T> __device__ __forceinline__ typename In<T>::vec narrow8(const f32x16 &v, int part)
+{
+    typedef __attribute__((__vector_size__(8 * sizeof(typename In<T>::out16)))) typename In<T>::out16 e8;
+    e8 o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = static_cast<typename In<T>::out16>(v[8 * part + i]);
+    return __builtin_bit_cast(typename In<T>::vec, o);
+}
+
+__device__ __forceinline__ f32x16 zero16()
+{
+    f32x16 z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    return z;
+}
+
+// The other half of the wavefront's value (lane ^ 32).
+template <class F> __device__ __forceinline__ float join_halves(float v, F &&f)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false);
+    return f(__builtin_bit_cast(float, (unsigned)a[0]), __builtin_bit_cast(float, (unsigned)a[1]));
+}
+
+// 32 consecutive columns of one row per lane pair (l, l ^ 32), from a 32 x 32 result whose column is the row (lane l % 32) and whose
+// rows are the columns: rounded, 16 bytes per store.  n: columns that exist (a multiple of 8).  rest: null, or where what the
+// rounding took goes, rounded in turn.
+template <class T> __device__ __forceinline__ void store_row32(char *p, const f32x16 &v, float mul, int n, bool live, char *rest = nullptr)
+{
+    using E = typename In<T>::out16;
+    typedef __attribute__((__vector_size__(4 * sizeof(E)))) E e4;
+    const int h = (threadIdx.x >> 5) & 1;
+    auto put = [&](char *to, e4 a, e4 b, int g) __attribute__((always_inline)) {
+        const uint2 x = __builtin_bit_cast(uint2, a), y = __builtin_bit_cast(uint2, b);
+        const auto s = __builtin_amdgcn_permlane32_swap(x.x, y.x, false, false), t = __builtin_amdgcn_permlane32_swap(x.y, y.y, false, false);
+        // the lower lane has columns 16 g .. 16 g + 7, the upper one the next eight
+        const int col = 16 * g + 8 * h;
+        if (live && col < n) *reinterpret_cast<uint4 *>(to + 2 * col) = make_uint4(s[0], t[0], s[1], t[1]);
+    };
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+        e4 a, b;                    // columns 16 g + 4 h .. and 16 g + 8 + 4 h ..
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a[i] = static_cast<E>(v[8 * g + i] * mul);
+            b[i] = static_cast<E>(v[8 * g + 4 + i] * mul);
+        }
+        put(p, a, b, g);
+        if (rest) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                a[i] = static_cast<E>(v[8 * g + i] * mul - static_cast<float>(a[i]));
+                b[i] = static_cast<E>(v[8 * g + 4 + i] * mul - static_cast<float>(b[i]));
+            }
+            put(rest, a, b, g);
+        }
+    }
+}
+
+}  // namespace
+
+inline bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// Checks a call and fills the parameters both directions share (SDROP_OK or an error).
+int attn_params(const sdrop_attn_t *a, bool backward, AttnParams &P);
+
+}  // namespace sdrop
+#endif

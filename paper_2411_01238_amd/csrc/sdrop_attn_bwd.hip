@@ -1,0 +1,357 @@
+// Attention, backward: the gradients of q, k and v from that of O.
+//
+//     P = exp(S - lse),  dP = dO V^T,  delta = row sums of dO O,  dS = P (dP - delta)
+//     dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO
+//
+// Scores are computed again from q, k and the forward pass's lse; nothing of their size is stored.  Two launches: dQ, a workgroup per
+// tile of rows that walks the keys (it has dO and O of its rows at hand and leaves lse and delta for the other), then dK and dV, a
+// workgroup per tile of keys that walks the rows of all query heads that share them.  Each gradient is summed in registers in
+// a fixed order: no atomics, results repeat bit for bit, at the price of computing S and dP twice (7 products instead of 5).
+#include "attn_common.h"
+#include <math.h>
+
+namespace sdrop {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+// dV's P is held as 256 P: over thousands of keys P itself would fall among fp16's smallest numbers, whose steps are coarse.  (The
+// factor is part of lse and delta and leaves dS as it is.)
+constexpr float kPShift = 8.f, kPScale = 1.f / 256.f;
+
+// Row r of (sequence b, key head hkv): its place among all rows' statistics.
+__device__ __forceinline__ int64_t stats_at(const AttnParams &P, const Sequence &s, int b, int hkv)
+{
+    return P.cu_q ? (s.q0 * P.Hkv + (int64_t)hkv * s.Lq) * P.G : ((int64_t)b * P.Hkv + hkv) * P.max_rows;
+}
+
+template <class T> __device__ __forceinline__ float dot8(uint4 a, uint4 b, float sum)
+{
+    typedef __attribute__((__vector_size__(8 * sizeof(typename In<T>::out16)))) typename In<T>::out16 e8;
+    const e8 x = __builtin_bit_cast(e8, a), y = __builtin_bit_cast(e8, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += static_cast<float>(x[i]) * static_cast<float>(y[i]);
+    return sum;
+}
+
+// dQ.  As in the forward pass a lane holds keys of one query: S^T = K Q^T, dP^T = V dO^T, dQ^T = K^T dS^T; lse and delta are one number
+// per lane each.
+template <class T, int HD>
+__global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams P)
+{
+    constexpr int TKV = 64, TILE = TKV * HD * 2, DB = HD / 32;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * TILE];
+    const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), h = lane >> 5;
+    int bh, unit;
+    place(P, P.tiles, bh, unit);
+    const int b = bh / P.Hkv, hkv = bh - b * P.Hkv, tile = P.tiles - 1 - unit;
+    const Sequence s = sequence_of(P, b);
+    if (!s.ok) return;
+    const int rows = s.Lq * P.G, R0 = tile * 128;
+    if (R0 >= rows) return;
+    const int off = s.Lk - s.Lq, r_last = min(R0 + 128, rows) - 1;
+    const int k_end = P.causal ? min(s.Lk, token_of(P, r_last) + off + 1) : s.Lk;
+    const int n_tiles = k_end > 0 ? (k_end + TKV - 1) / TKV : 0;
+
+    const int w0 = R0 + 32 * wave, r = w0 + (lane & 31);
+    const bool live = r < rows;
+    const int i = token_of(P, min(r, rows - 1)), head = hkv * P.G + (min(r, rows - 1) - i * P.G);
+    const int lim = !live ? -1 : P.causal ? min(s.Lk - 1, i + off) : s.Lk - 1;
+    const bool any = w0 < rows;
+    const int w_first = any ? uni(token_of(P, w0)) + off : 0, w_last = any ? uni(token_of(P, min(w0 + 31, rows - 1))) + off : -1;
+
+    typename In<T>::vec qf[HD / 16], gf[HD / 16];
+    float delta = 0.f;
+    {
+        const char *const qp = P.q + (P.cu_q ? 0 : b * P.q_b) + (s.q0 + i) * P.q_t + head * P.q_h;
+        const char *const gp = P.dout + (P.cu_q ? 0 : b * P.do_b) + (s.q0 + i) * P.do_t + head * P.do_h;
+        const int64_t at = (P.cu_q ? 0 : b * P.o_b) + (s.q0 + i) * P.o_t + head * P.o_h;
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+            const int col = 16 * kk + 8 * h;
+            uint4 x = make_uint4(0, 0, 0, 0), g = x, o = x, rest = x;
+            if (live && col < P.D) {
+                x = *reinterpret_cast<const uint4 *>(qp + 2 * col);
+                g = *reinterpret_cast<const uint4 *>(gp + 2 * col);
+                o = *reinterpret_cast<const uint4 *>(P.o + at + 2 * col);
+                if (P.rest) rest = *reinterpret_cast<const uint4 *>(P.rest + at + 2 * col);
+            }
+            qf[kk] = __builtin_bit_cast(typename In<T>::vec, x);
+            gf[kk] = __builtin_bit_cast(typename In<T>::vec, g);
+            delta = dot8<T>(g, rest, dot8<T>(g, o, delta));
+        }
+    }
+    delta = join_halves(delta, [](float a, float c) { return a + c; });
+    // (a row that saw no key: +inf makes every P of it 0)
+    float lse2 = INFINITY;
+    if (live) {
+        const float x = P.lse[P.cu_q ? head * P.total_q + s.q0 + i : ((int64_t)b * P.Hq + head) * P.max_q + i];
+        if (x != -INFINITY) lse2 = x * kLog2e;
+        if (h == 0) reinterpret_cast<float2 *>(P.delta)[stats_at(P, s, b, hkv) + r] = make_float2(lse2, delta);
+    }
+
+    f32x16 acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[d] = zero16();
+    const char *kb = P.k + (P.cu_k ? 0 : b * P.k_b) + s.k0 * P.k_t + hkv * P.k_h;
+    const char *vb = P.v + (P.cu_k ? 0 : b * P.v_b) + s.k0 * P.v_t + hkv * P.v_h;
+    const int nch = P.D / 8;
+    TileLoad<HD, TKV, 4> lk, lv;
+    lk.init(P.k_t, wave);
+    lv.init(P.v_t, wave);
+    auto request = [&](int t, int buf) __attribute__((always_inline)) {
+        const int left = s.Lk - t * TKV;
+        lk.issue(kb, P.k_t, lds + buf * 2 * TILE, left, nch);
+        lv.issue(vb, P.v_t, lds + buf * 2 * TILE + TILE, left, nch);
+        kb += TKV * P.k_t;
+        vb += TKV * P.v_t;
+    };
+    if (n_tiles > 0) request(0, 0);
+    for (int t = 0; t < n_tiles; ++t) {
+        const int buf = t & 1;
+        landed();
+        if (t + 1 < n_tiles) request(t + 1, buf ^ 1);
+        const int kv0 = t * TKV;
+        if (P.causal && kv0 > w_last) continue;
+        const char *const kt = lds + buf * 2 * TILE, *const vt = kt + TILE;
+        const bool masked = kv0 + TKV > s.Lk || (P.causal && kv0 + TKV - 1 > w_first);
+        // (one block of 32 keys after the other: the registers of two do not fit beside Q, dO and dQ)
+#pragma unroll 1
+        for (int mb = 0; mb < 2; ++mb) {
+            const RowOperand<HD, T> ka(kt + mb * 64 * HD), va(vt + mb * 64 * HD);
+            const ColOperand<HD, T> kc(kt + mb * 64 * HD);
+            f32x16 sc = zero16(), dp = zero16();
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk) sc = In<T>::mfma(ka.get(0, kk), qf[kk], sc);
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk) dp = In<T>::mfma(va.get(0, kk), gf[kk], dp);
+            if (masked) {
+                const int last = lim - kv0 - 32 * mb - 4 * h;
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (8 * (e >> 2) + (e & 3) > last) sc[e] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[e] = __builtin_amdgcn_exp2f(sc[e] * P.c - lse2) * (dp[e] - delta);
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                const typename In<T>::vec ds = narrow8<T>(sc, ks);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) acc[d] = In<T>::mfma(kc.get(d, ks), ds, acc[d]);
+            }
+        }
+    }
+    char *const dst = P.dq + (P.cu_q ? 0 : b * P.dq_b) + (s.q0 + i) * P.dq_t + head * P.dq_h;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) store_row32<T>(dst + 64 * d, acc[d], P.scale, P.D - 32 * d, live);
+}
+
+// dK and dV.  A wavefront owns 32 keys; a lane holds rows (queries) of one key: S = Q K^T, dP = dO V^T, dV^T = dO^T P, dK^T = Q^T dS.
+template <class T, int HD>
+__global__ __launch_bounds__(256, HD <= 64 ? 2 : 1) void attn_dkv_kernel(AttnParams P)
+{
+    constexpr int TQ = 64, TILE = TQ * HD * 2, DB = HD / 32;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * TILE];
+    __shared__ float st_lse[2][TQ], st_delta[2][TQ];
+    __shared__ int st_lim[2][TQ];                   // last key that the row sees
+    const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), h = lane >> 5;
+    int bh, unit;
+    place(P, P.tiles, bh, unit);
+    const int b = bh / P.Hkv, hkv = bh - b * P.Hkv, K0 = unit * 128;
+    const Sequence s = sequence_of(P, b);
+    if (!s.ok) return;
+    // rows of dK and dV that this call writes; behind a dense sequence's last key they are 0
+    const int out_rows = P.cu_k ? s.Lk : P.max_k;
+    if (K0 >= out_rows) return;
+    const int rows = K0 < s.Lk ? s.Lq * P.G : 0, off = s.Lk - s.Lq;
+    // causal: the first row that sees a key of this tile
+    const int r_first = P.causal ? min(max(K0 - off, 0), s.Lq) * P.G : 0;
+    const int t0 = r_first / TQ, t1 = (rows + TQ - 1) / TQ;
+
+    const int w0 = K0 + 32 * wave, key = w0 + (lane & 31);
+    const bool live = key < s.Lk;
+    typename In<T>::vec kf[HD / 16], vf[HD / 16];
+    {
+        const int64_t at = s.k0 + min(key, max(s.Lk - 1, 0));
+        const char *const kp = P.k + (P.cu_k ? 0 : b * P.k_b) + at * P.k_t + hkv * P.k_h;
+        const char *const vp = P.v + (P.cu_k ? 0 : b * P.v_b) + at * P.v_t + hkv * P.v_h;
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+            const int col = 16 * kk + 8 * h;
+            uint4 x = make_uint4(0, 0, 0, 0), y = x;
+            if (live && col < P.D) {
+                x = *reinterpret_cast<const uint4 *>(kp + 2 * col);
+                y = *reinterpret_cast<const uint4 *>(vp + 2 * col);
+            }
+            kf[kk] = __builtin_bit_cast(typename In<T>::vec, x);
+            vf[kk] = __builtin_bit_cast(typename In<T>::vec, y);
+        }
+    }
+    f32x16 dk[DB], dv[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zero16();
+
+    const char *const qb = P.q + (P.cu_q ? 0 : b * P.q_b) + s.q0 * P.q_t + (int64_t)hkv * P.G * P.q_h;
+    const char *const gb = P.dout + (P.cu_q ? 0 : b * P.do_b) + s.q0 * P.do_t + (int64_t)hkv * P.G * P.do_h;
+    const float2 *const stats = reinterpret_cast<const float2 *>(P.delta) + stats_at(P, s, b, hkv);
+    const int nch = P.D / 8;
+    // rows of a tile are tokens and heads of the group in turn: each lane works out where its rows lie
+    constexpr int ROW_BYTES = 2 * HD, RPI = 1024 / ROW_BYTES, PASSES = TQ / (RPI * 4);
+    const int lrow = RPI * wave + (lane * 16) / ROW_BYTES, chunk = ((lane * 16) % ROW_BYTES >> 4) ^ swz_a<HD>(lrow);
+    auto request = [&](int t, int buf) __attribute__((always_inline)) {
+        char *const dst = lds + buf * 2 * TILE;
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int rr = t * TQ + lrow + RPI * 4 * p;
+            char *const at = dst + (wave + 4 * p) * 1024;
+            if (rr < rows && chunk < nch) {
+                const int tok = token_of(P, rr), g = rr - tok * P.G;
+                dma16_at(qb + tok * P.q_t + g * P.q_h + chunk * 16, at);
+                dma16_at(gb + tok * P.do_t + g * P.do_h + chunk * 16, at + TILE);
+            } else {
+                *reinterpret_cast<uint4 *>(at + lane * 16) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>(at + TILE + lane * 16) = make_uint4(0, 0, 0, 0);
+            }
+        }
+    };
+    // A tile's statistics go through a register: asked for with the tile, put into LDS when the tile before it has been computed
+    // (the compiler's own wait for them would otherwise be one for the whole tile).
+    float2 next = make_float2(INFINITY, 0.f);
+    auto ask = [&](int t) __attribute__((always_inline)) {
+        const int rr = t * TQ + (int)threadIdx.x;
+        next = threadIdx.x < TQ && rr < rows ? stats[rr] : make_float2(INFINITY, 0.f);
+    };
+    auto put = [&](int t, int buf) __attribute__((always_inline)) {
+        if (threadIdx.x < TQ) {
+            const int rr = t * TQ + (int)threadIdx.x;
+            st_lse[buf][threadIdx.x] = next.x - kPShift;
+            st_delta[buf][threadIdx.x] = next.y * kPScale;
+            st_lim[buf][threadIdx.x] = rr < rows ? token_of(P, rr) + off : -1;
+        }
+    };
+    if (t0 < t1) {
+        ask(t0);
+        request(t0, 0);
+        put(t0, 0);
+    }
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1;
+        landed();
+        if (t + 1 < t1) {
+            ask(t + 1);
+            request(t + 1, buf ^ 1);
+        }
+        const char *const qt = lds + buf * 2 * TILE, *const gt = qt + TILE;
+        const RowOperand<HD, T> qa(qt), ga(gt);
+        const ColOperand<HD, T> qc(qt), gc(gt);
+#pragma unroll
+        for (int mb = 0; mb < 2; ++mb) {
+            const int rb = t * TQ + 32 * mb;
+            if (rb >= rows) continue;
+            const int see_first = P.causal ? uni(token_of(P, rb)) + off : s.Lk, see_last = P.causal ? uni(token_of(P, min(rb + 31, rows - 1))) + off : s.Lk;
+            if (see_last < w0) continue;            // none of these rows sees a key of this wavefront
+            f32x16 sc = zero16(), dp = zero16();
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk) sc = In<T>::mfma(qa.get(32 * mb, kk), kf[kk], sc);
+#pragma unroll
+            for (int kk = 0; kk < HD / 16; ++kk) dp = In<T>::mfma(ga.get(32 * mb, kk), vf[kk], dp);
+            if (P.causal && see_first < w0 + 31) {
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (key > st_lim[buf][32 * mb + 8 * g + 4 * h + e]) sc[4 * g + e] = -INFINITY;
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32q l4 = *reinterpret_cast<const f32q *>(&st_lse[buf][32 * mb + 8 * g + 4 * h]);
+                const f32q d4 = *reinterpret_cast<const f32q *>(&st_delta[buf][32 * mb + 8 * g + 4 * h]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(sc[4 * g + e] * P.c - l4[e]);
+                    sc[4 * g + e] = p;
+                    dp[4 * g + e] = p * (dp[4 * g + e] * kPScale - d4[e]);
+                }
+            }
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                const typename In<T>::vec p = narrow8<T>(sc, ks), ds = narrow8<T>(dp, ks);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) dv[d] = In<T>::mfma(gc.get(d, 2 * mb + ks), p, dv[d]);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) dk[d] = In<T>::mfma(qc.get(d, 2 * mb + ks), ds, dk[d]);
+            }
+        }
+        if (t + 1 < t1) put(t + 1, buf ^ 1);
+    }
+    if (!live) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zero16();
+    }
+    const bool write = key < out_rows;
+    char *const dkp = P.dk + (P.cu_k ? 0 : b * P.dk_b) + (s.k0 + key) * P.dk_t + hkv * P.dk_h;
+    char *const dvp = P.dv + (P.cu_k ? 0 : b * P.dv_b) + (s.k0 + key) * P.dv_t + hkv * P.dv_h;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+        store_row32<T>(dkp + 64 * d, dk[d], P.scale, P.D - 32 * d, write);
+        store_row32<T>(dvp + 64 * d, dv[d], kPScale, P.D - 32 * d, write);
+    }
+}
+
+template <class T, int HD> int launch_bwd(AttnParams P, hipStream_t st)
+{
+    P.tiles = (P.max_rows + 127) / 128;
+    hipLaunchKernelGGL((attn_dq_kernel<T, HD>), dim3((unsigned)((int64_t)P.B * P.Hkv * P.tiles)), dim3(256), 0, st, P);
+    const int rc = hip_status(hipGetLastError());
+    if (rc != SDROP_OK) return rc;
+    P.tiles = (P.max_k + 127) / 128;
+    hipLaunchKernelGGL((attn_dkv_kernel<T, HD>), dim3((unsigned)((int64_t)P.B * P.Hkv * P.tiles)), dim3(256), 0, st, P);
+    return hip_status(hipGetLastError());
+}
+
+size_t stats_bytes(const AttnParams &P)
+{
+    return (P.cu_q ? (size_t)P.total_q * P.Hq : (size_t)P.B * P.Hkv * P.max_rows) * 2 * sizeof(float);
+}
+
+}  // namespace
+}  // namespace sdrop
+
+using namespace sdrop;
+
+extern "C" {
+
+size_t sdrop_attn_bwd_workspace_bytes(const sdrop_attn_t *a)
+{
+    AttnParams P;
+    return attn_params(a, true, P) == SDROP_OK ? stats_bytes(P) : 0;
+}
+
+int sdrop_attn_bwd(const void *dO, const void *q, const void *k, const void *v, const void *o, const void *o_rest, const float *lse,
+                   void *dq, void *dk, void *dv, const sdrop_attn_t *a, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!dO || !q || !k || !v || !o || !lse || !dq || !dk || !dv) return SDROP_EINVAL;
+    AttnParams P;
+    const int rc = attn_params(a, true, P);
+    if (rc != SDROP_OK) return rc;
+    if (!aligned16(dO) || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(o_rest) || !aligned16(dq) || !aligned16(dk) ||
+        !aligned16(dv) || reinterpret_cast<uintptr_t>(lse) % 4) return SDROP_EALIGN;
+    if (!ws || ws_bytes < stats_bytes(P) || !aligned16(ws)) return SDROP_EWORKSPACE;
+    const int64_t most = (int64_t(1) << 24) - 1, heads = (int64_t)P.B * P.Hkv;      // (a launch counts its threads in 32 bits)
+    if (heads * ((P.max_rows + 127) / 128) > most || heads * (((int64_t)P.max_k + 127) / 128) > most) return SDROP_ESHAPE;
+    P.dout = static_cast<const char *>(dO);
+    P.q = static_cast<const char *>(q);
+    P.k = static_cast<const char *>(k);
+    P.v = static_cast<const char *>(v);
+    P.o = static_cast<const char *>(o);
+    P.rest = static_cast<const char *>(o_rest);
+    P.lse = const_cast<float *>(lse);
+    P.dq = static_cast<char *>(dq);
+    P.dk = static_cast<char *>(dk);
+    P.dv = static_cast<char *>(dv);
+    P.delta = static_cast<float *>(ws);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (a->dtype == SDROP_F16) return P.D <= 64 ? launch_bwd<F16, 64>(P, st) : launch_bwd<F16, 128>(P, st);
+    return P.D <= 64 ? launch_bwd<BF16, 64>(P, st) : launch_bwd<BF16, 128>(P, st);
+}
+
+}  // extern "C"

@@ -28,7 +28,8 @@ EXPORTS = ("sdrop_strerror", "sdrop_last_hip_error", "sdrop_status", "sdrop_set_
            "sdrop_bwd", "sdrop_bwd_ex", "sdrop_fwd_ex", "sdrop_bwd_dx_ex", "sdrop_bwd_dw_ex", "sdrop_workspace_bytes_ex",
            "sdrop_producer", "sdrop_producer_ex", "sdrop_producer_zeroed", "sdrop_bwd_gated", "sdrop_producer_bwd",
            "sdrop_bias_grad_workspace_bytes", "sdrop_bias_grad", "sdrop_col_sum_workspace_bytes", "sdrop_col_sum",
-           "sdrop_dropout", "sdrop_layer_norm", "sdrop_layer_norm_bwd_workspace_bytes", "sdrop_layer_norm_bwd")
+           "sdrop_dropout", "sdrop_layer_norm", "sdrop_layer_norm_bwd_workspace_bytes", "sdrop_layer_norm_bwd",
+           "sdrop_attn_workspace_bytes", "sdrop_attn", "sdrop_attn_bwd_workspace_bytes", "sdrop_attn_bwd")
 
 SCALE_DROPOUT, SCALE_ONE = 0, 1
 ACT_NONE, ACT_RELU, ACT_GELU_TANH, ACT_GELU_ERF = 0, 1, 2, 3
@@ -57,6 +58,14 @@ class Epilogue(ctypes.Structure):
                 ("bias", ctypes.c_void_p), ("relu_mask", ctypes.c_void_p),
                 ("ld_a", ctypes.c_int64), ("ld_b", ctypes.c_int64), ("ld_out", ctypes.c_int64),
                 ("gate_mode", ctypes.c_int32), ("w_layout", ctypes.c_int32), ("kept_fraction", ctypes.c_double)]
+
+
+class Attn(ctypes.Structure):
+    """sdrop_attn_t of the header."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("B", "max_q", "max_k", "Hq", "Hkv", "D", "total_q", "total_k")] +
+                [(n, ctypes.c_void_p) for n in ("cu_q", "cu_k", "k_len")] +
+                [(n + s, ctypes.c_int64) for n in ("q", "k", "v", "o", "do", "dq", "dk", "dv") for s in ("_b", "_t", "_h")] +
+                [("scale", ctypes.c_double), ("causal", ctypes.c_int32), ("dtype", ctypes.c_int32)])
 
 
 _lib = None
@@ -146,6 +155,14 @@ def lib():
         L.sdrop_layer_norm_bwd_workspace_bytes.restype = sz
         L.sdrop_layer_norm_bwd.argtypes = [vp] * 10 + [i64, i64, dbl, u64, u64, ci, ci, i64, i64, i64, i64, i64, vp, sz, vp]
         L.sdrop_layer_norm_bwd.restype = ci
+        L.sdrop_attn_workspace_bytes.argtypes = [ctypes.POINTER(Attn)]
+        L.sdrop_attn_workspace_bytes.restype = sz
+        L.sdrop_attn.argtypes = [vp, vp, vp, vp, vp, vp, ctypes.POINTER(Attn), vp, sz, vp]
+        L.sdrop_attn.restype = ci
+        L.sdrop_attn_bwd_workspace_bytes.argtypes = [ctypes.POINTER(Attn)]
+        L.sdrop_attn_bwd_workspace_bytes.restype = sz
+        L.sdrop_attn_bwd.argtypes = [vp] * 10 + [ctypes.POINTER(Attn), vp, sz, vp]
+        L.sdrop_attn_bwd.restype = ci
         _lib = L
     return _lib
 
@@ -164,6 +181,7 @@ def set_tuning(knob, value):
 
 
 STATUS_MASK_MISMATCH = 1
+STATUS_BAD_LENGTHS = 2
 
 
 def status(clear=True):
@@ -841,3 +859,109 @@ def sdrop_layer_norm_bwd(dY, H, gamma, mean, rstd, dH=None, p=0.0, seed=0, rng_s
                                       dt, _DTYPES[gamma.dtype], ldy, lddh, ldh, 0, 0, None if ws is None else ws.data_ptr(),
                                       0 if ws is None else ws.numel() * ws.element_size(), _stream()), "sdrop_layer_norm_bwd")
     return (dx if drops else dr if need_dx else None), (dr if need_dr else None), dg, db
+
+
+# ---- attention ----
+
+def _heads(t, name, lead, heads, D, dtype):
+    """Address and strides (sequence, token, head; elements) of [B, T, H, D] or, packed, [tokens, H, D]."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.dim() == len(lead) + 2):
+        raise ValueError("%s must be a GPU tensor [%s, heads, D] of the queries' dtype" % (name, "B, tokens" if len(lead) == 2 else "tokens"))
+    if tuple(t.shape) != tuple(lead) + (heads, D):
+        raise SdropError(ESHAPE, "attention: the shape of %s" % name)
+    if t.stride(-1) != 1 and D > 1:
+        raise ValueError("the last dimension of %s must be contiguous" % name)
+    # (a dimension of size 1 has no stride worth the name)
+    s = [0 if n == 1 else st for n, st in zip(t.shape[:-1], t.stride()[:-1])]
+    return t.data_ptr(), [0] * (3 - len(s)) + s
+
+
+def _index(t, name, n):
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) != (n,):
+        raise ValueError("%s must be int32 with %d values" % (name, n))
+    return _dev(t, name)
+
+
+def _attn_desc(q, k, v, causal, scale, cu_q, cu_k, max_q, max_k, k_len):
+    """The description of a call, and the addresses of q, k and v.  Packed queries and keys come as [tokens, heads, D]."""
+    if not (isinstance(q, torch.Tensor) and isinstance(k, torch.Tensor)):
+        raise ValueError("q and k must be tensors")
+    if q.dtype not in (torch.float16, torch.bfloat16):
+        raise SdropError(EDTYPE, "attention")
+    if q.dim() != (4 if cu_q is None else 3) or k.dim() != (4 if cu_k is None else 3):
+        raise ValueError("q and k are [B, tokens, heads, D], or [tokens, heads, D] where their offsets are given")
+    if (cu_q is not None and max_q is None) or (cu_k is not None and max_k is None):
+        raise ValueError("packed sequences need an upper bound of their lengths (max_q, max_k)")
+    Hq, D = q.shape[-2:]
+    Hkv = k.shape[-2]
+    B = q.shape[0] if cu_q is None else cu_q.shape[0] - 1
+    a = Attn(B=B, Hq=Hq, Hkv=Hkv, D=D, max_q=q.shape[1] if cu_q is None else int(max_q), max_k=k.shape[1] if cu_k is None else int(max_k),
+             total_q=0 if cu_q is None else q.shape[0], total_k=0 if cu_k is None else k.shape[0],
+             cu_q=_index(cu_q, "cu_q", B + 1), cu_k=_index(cu_k, "cu_k", B + 1), k_len=_index(k_len, "k_len", B),
+             scale=D ** -0.5 if scale is None else float(scale), causal=1 if causal else 0, dtype=_DTYPES[q.dtype])
+    lead_k = (B, k.shape[1]) if cu_k is None else (k.shape[0],)
+    pq, (a.q_b, a.q_t, a.q_h) = _heads(q, "q", q.shape[:-2], Hq, D, q.dtype)
+    pk, (a.k_b, a.k_t, a.k_h) = _heads(k, "k", lead_k, Hkv, D, q.dtype)
+    pv, (a.v_b, a.v_t, a.v_h) = _heads(v, "v", lead_k, Hkv, D, q.dtype)
+    return a, pq, pk, pv
+
+
+def sdrop_attn(q, k, v, causal=False, scale=None, cu_q=None, cu_k=None, max_q=None, max_k=None, k_len=None, out=None, need_lse=True, need_rest=False,
+               ws=None):
+    """O = softmax(scale q k^T) v per head (scale: D ** -0.5 if not given); returns (O, lse), lse the fp32 log-sum-exp of the scores
+    that the backward pass needs: [B, Hq, Tq], packed [Hq, tokens] (None with need_lse=False).  need_rest: (O, lse, rest), rest what
+    O's rounding took, rounded in turn; the backward pass is the more exact for it.
+
+    q [B, Tq, Hq, D], k and v [B, Tk, Hkv, D] in fp16 or bf16, Hq a multiple of Hkv, D a multiple of 8 up to 128, any strides that keep
+    16-byte alignment and contiguous D.  causal: token i sees keys up to i + Lk - Lq.  cu_q / cu_k: int32 offsets [B + 1] of packed
+    sequences in [tokens, heads, D], with max_q / max_k bounding their lengths.  k_len: int32 [B], how many of the Tk keys there are."""
+    a, pq, pk, pv = _attn_desc(q, k, v, causal, scale, cu_q, cu_k, max_q, max_k, k_len)
+    if out is None:
+        # (rows behind the last packed sequence are not written)
+        out = (torch.empty if cu_q is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+    po, (a.o_b, a.o_t, a.o_h) = _heads(out, "out", q.shape[:-2], a.Hq, a.D, q.dtype)
+    rest = torch.empty_strided(out.shape, out.stride(), dtype=q.dtype, device=q.device) if need_rest else None
+    lse = None
+    if need_lse:
+        lse = torch.empty((a.B, a.Hq, a.max_q) if cu_q is None else (a.Hq, a.total_q), dtype=torch.float32, device=q.device)
+    _on_current_device(q)
+    L = lib()
+    ref = ctypes.byref(a)
+    need = L.sdrop_attn_workspace_bytes(ref)
+    if ws is None and need:
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(L.sdrop_attn(pq, pk, pv, po, None if rest is None else rest.data_ptr(), None if lse is None else lse.data_ptr(), ref,
+                        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel() * ws.element_size(), _stream()), "sdrop_attn")
+    return (out, lse, rest) if need_rest else (out, lse)
+
+
+def sdrop_attn_bwd(dO, q, k, v, O, lse, causal=False, scale=None, cu_q=None, cu_k=None, max_q=None, max_k=None, k_len=None,
+                   rest=None, out_dq=None, out_dk=None, out_dv=None, ws=None):
+    """The gradients (dq, dk, dv) of sdrop_attn, from its O, lse and (if kept) rest; the other arguments as in that call."""
+    a, pq, pk, pv = _attn_desc(q, k, v, causal, scale, cu_q, cu_k, max_q, max_k, k_len)
+    lead_q, lead_k = q.shape[:-2], k.shape[:-2]
+    if lse.dtype != torch.float32 or tuple(lse.shape) != ((a.B, a.Hq, a.max_q) if cu_q is None else (a.Hq, a.total_q)):
+        raise ValueError("lse must be the fp32 tensor that sdrop_attn returned")
+    new = lambda t, cu: (torch.empty if cu is None else torch.zeros)(t.shape, dtype=q.dtype, device=q.device)     # noqa: E731
+    out_dq = new(q, cu_q) if out_dq is None else out_dq
+    out_dk = new(k, cu_k) if out_dk is None else out_dk
+    out_dv = new(k, cu_k) if out_dv is None else out_dv
+    pg, (a.do_b, a.do_t, a.do_h) = _heads(dO, "dO", lead_q, a.Hq, a.D, q.dtype)
+    po, so = _heads(O, "O", lead_q, a.Hq, a.D, q.dtype)
+    a.o_b, a.o_t, a.o_h = so
+    pr, sr = (None, so) if rest is None else _heads(rest, "rest", lead_q, a.Hq, a.D, q.dtype)
+    if sr != so:
+        raise ValueError("rest must have O's strides")
+    pdq, (a.dq_b, a.dq_t, a.dq_h) = _heads(out_dq, "out_dq", lead_q, a.Hq, a.D, q.dtype)
+    pdk, (a.dk_b, a.dk_t, a.dk_h) = _heads(out_dk, "out_dk", lead_k, a.Hkv, a.D, q.dtype)
+    pdv, (a.dv_b, a.dv_t, a.dv_h) = _heads(out_dv, "out_dv", lead_k, a.Hkv, a.D, q.dtype)
+    _on_current_device(q)
+    L = lib()
+    ref = ctypes.byref(a)
+    if ws is None:
+        ws = torch.empty(max(L.sdrop_attn_bwd_workspace_bytes(ref), 16), dtype=torch.uint8, device=q.device)
+    _check(L.sdrop_attn_bwd(pg, pq, pk, pv, po, pr, _dev(lse, "lse"), pdq, pdk, pdv, ref, ws.data_ptr(), ws.numel() * ws.element_size(),
+                            _stream()), "sdrop_attn_bwd")
+    return out_dq, out_dk, out_dv

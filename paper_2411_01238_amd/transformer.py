@@ -22,6 +22,15 @@ def _grad_rows(g):
     return g if g.shape[0] == 1 or g.stride(0) >= g.shape[1] else g.contiguous()
 
 
+def _once(backward):
+    """once_differentiable, whose own work (a third of a small backward's host time) is left out where no graph is asked for."""
+    with_graph = torch.autograd.function.once_differentiable(backward)
+
+    def call(ctx, *grads):
+        return (with_graph if torch.is_grad_enabled() else backward)(ctx, *grads)
+    return call
+
+
 class _Dropout(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, p, seed, rng_stream):
@@ -30,7 +39,7 @@ class _Dropout(torch.autograd.Function):
         return y.view(x.shape)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy):
         dx = sdrop.sdrop_dropout(_grad_rows(dy), *ctx.args).view(dy.shape) if ctx.needs_input_grad[0] else None
         return dx, dy if ctx.needs_input_grad[1] else None, None, None, None
@@ -53,7 +62,7 @@ class _LayerNorm(torch.autograd.Function):
         return y.view(x.shape)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy):
         h, weight, mean, rstd = ctx.saved_tensors
         nx, nw, nb = ctx.needs_input_grad[:3]
@@ -77,7 +86,7 @@ class _DropoutAddNorm(torch.autograd.Function):
         return y.view(x.shape), h.view(x.shape)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, dy, dh):
         h, weight, mean, rstd = ctx.saved_tensors
         p, seed, rng_stream = ctx.args
@@ -98,6 +107,37 @@ def dropout_add_norm(x, residual, weight, bias=None, p=0.0, eps=1e-5, seed=0, rn
     if residual.shape != x.shape:
         raise ValueError("residual must have x's shape")
     return _DropoutAddNorm.apply(x, residual, weight, bias, float(p), float(eps), int(seed), int(rng_stream))
+
+
+def _last_contiguous(t):
+    # (what the kernels take in place: contiguous heads, 16-byte steps; anything else is copied once)
+    ok = t.stride(-1) == 1 and all(n == 1 or (s > 0 and s % 8 == 0) for n, s in zip(t.shape[:-1], t.stride()[:-1])) and t.data_ptr() % 16 == 0
+    return t if ok else t.contiguous()
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, causal, scale, cu_q, cu_k, max_q, max_k, k_len):
+        q, k, v = _last_contiguous(q), _last_contiguous(k), _last_contiguous(v)
+        if not any(ctx.needs_input_grad[:3]):
+            return sdrop.sdrop_attn(q, k, v, causal, scale, cu_q, cu_k, max_q, max_k, k_len, need_lse=False)[0]
+        o, lse, rest = sdrop.sdrop_attn(q, k, v, causal, scale, cu_q, cu_k, max_q, max_k, k_len, need_rest=True)
+        ctx.save_for_backward(q, k, v, o, lse, rest, cu_q, cu_k, k_len)
+        ctx.args = (causal, scale, max_q, max_k)
+        return o
+
+    @staticmethod
+    @_once
+    def backward(ctx, do):
+        q, k, v, o, lse, rest, cu_q, cu_k, k_len = ctx.saved_tensors
+        causal, scale, max_q, max_k = ctx.args
+        dq, dk, dv = sdrop.sdrop_attn_bwd(_last_contiguous(do), q, k, v, o, lse, causal, scale, cu_q, cu_k, max_q, max_k, k_len, rest)
+        return dq, dk, dv, None, None, None, None, None, None, None
+
+
+def attention(q, k, v, causal=False, scale=None, cu_q=None, cu_k=None, max_q=None, max_k=None, k_len=None):
+    """softmax(scale q k^T) v per head; see sdrop.sdrop_attn for shapes, packed sequences, grouped heads and k_len."""
+    return _Attention.apply(q, k, v, bool(causal), scale, cu_q, cu_k, max_q, max_k, k_len)
 
 
 class ElementDropout(torch.nn.Module):

@@ -50,3 +50,26 @@ def test_layer_norm_gradients_against_differences():
     for i in range(13):
         assert dg[i] == pytest.approx(_difference(lambda t: (orc.layer_norm(h, t, b, 1e-5)[0] * dy).sum(), g, i, 1e-5), abs=1e-7)
         assert db[i] == pytest.approx(_difference(lambda t: (orc.layer_norm(h, g, t, 1e-5)[0] * dy).sum(), b, i, 1e-5), abs=1e-7)
+
+
+@pytest.mark.parametrize("Tq,Tk,causal", [(5, 5, True), (4, 7, True), (6, 3, True), (3, 4, False), (1, 6, True)])
+def test_attention_and_its_gradients_against_differences(Tq, Tk, causal):
+    r = np.random.RandomState(1)
+    q, k, v, do = r.randn(Tq, 4, 3), r.randn(Tk, 2, 3), r.randn(Tk, 2, 3), r.randn(Tq, 4, 3)
+    o, lse = orc.attention(q, k, v, 0.7, causal)
+    for i in range(Tq):
+        n = min(Tk, i + Tk - Tq + 1) if causal else Tk
+        if n <= 0:
+            assert not o[i].any() and np.all(np.isneginf(lse[:, i]))
+            continue
+        s = 0.7 * np.einsum("hd,jd->hj", q[i, :2], k[:n, 0])            # the first two query heads read the first key head
+        assert np.allclose(lse[:2, i], np.log(np.exp(s).sum(axis=1)))
+        assert np.allclose(o[i, :2], np.exp(s) / np.exp(s).sum(axis=1, keepdims=True) @ v[:n, 0])
+    grads = orc.attention_bwd(do, q, k, v, 0.7, causal)
+    for which, (x, g) in enumerate(zip((q, k, v), grads)):
+        def f(t, which=which):
+            a = [q, k, v]
+            a[which] = t
+            return (orc.attention(*a, 0.7, causal)[0] * do).sum()
+        for i in range(x.size):
+            assert g.flat[i] == pytest.approx(_difference(f, x, i, 1e-6), abs=1e-7)
