@@ -72,32 +72,49 @@ __device__ __forceinline__ int token_of(const AttnParams &P, int r)
     return (int)((__umulhi((uint32_t)r, P.g_mul) + (uint32_t)r) >> P.g_shift);
 }
 
-// Workgroup id -> (sequence and key head, unit).  Consecutive workgroups go to the eight XCDs in turn: eight heads at a time, one
-// for each XCD, so that the workgroups that read the same keys share an L2.
+// Workgroup id -> (sequence and key head, unit).  Consecutive workgroups go to the eight XCDs in turn.
+// Where all units cost the same: eight heads at a time, one for each XCD, so that the workgroups that read the same keys share
+// an L2.  Where they do not (a causal mask, sequences of different lengths): the first unit of every head, then the second, the
+// costly units being the first ones.  A head's units one after the other would start the last heads' costly ones
+// late (forward, 2 x 4096 tokens, 16 heads of 128, causal: 247 us against 190).
 __device__ __forceinline__ void place(const AttnParams &P, int units, int &bh, int &unit)
 {
     const int n = P.B * P.Hkv, id = blockIdx.x;
-    const int g = id / (8 * units), rem = id - g * 8 * units;
-    const int here = n - 8 * g < 8 ? n - 8 * g : 8;
-    bh = uni(8 * g + rem % here);
-    unit = uni(rem / here);
+    if (P.causal || P.cu_q || P.cu_k || P.k_len) {
+        unit = uni(id / n);
+        bh = uni(id - unit * n);
+    } else {
+        const int g = id / (8 * units), rem = id - g * 8 * units;
+        const int here = n - 8 * g < 8 ? n - 8 * g : 8;
+        bh = uni(8 * g + rem % here);
+        unit = uni(rem / here);
+    }
 }
 
-// ---- tiles in LDS: [rows][HD] of 16-bit values, as they lie in memory ----
+// ---- tiles in LDS: [rows][HD] of 16-bit values ----
 //
-// 16-byte chunk c of row r lies in slot c ^ swz_a(r).  Operands are read along the rows (ds_read_b128: 16 consecutive rows, one
-// chunk) and across them (ds_read_b64_tr_b16: 4 consecutive rows x 64 bytes); the value puts the former on all banks and the
-// rows of the latter 64 bytes apart.  It is the same for every 16 rows.
-template <int HD> __device__ __forceinline__ int swz_a(int r)
+// One load instruction of a wavefront fills 1 KiB, 4 rows of 128 values or 8 of 64; such groups lie 1040 bytes apart.  In a group 16-byte
+// chunk c of row r lies in slot c ^ swz_a(r).  Operands are read along the rows (ds_read_b128: 16 consecutive rows, one chunk) and
+// across them (ds_read_b64_tr_b16: 4 consecutive rows x 64 bytes): the XOR keeps the rows of a group apart and the 16 bytes between groups
+// the groups, so that either read is spread over all banks (no conflicts, counted).  An XOR of all 16 rows' bits would do the same
+// without the gap, but leave twice as many lane addresses to be made or kept.
+template <int HD> constexpr int tile_bytes(int rows) { return rows * HD / 512 * 1040; }
+template <int HD> __device__ __forceinline__ constexpr int swz_a(int r)
 {
-    return HD >= 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    return HD >= 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1;
+}
+// byte offset of row r (without its chunk)
+template <int HD> __device__ __forceinline__ constexpr int row_at(int r)
+{
+    constexpr int G = 512 / HD;
+    return r / G * 1040 + r % G * 2 * HD;
 }
 
 // Loads a tile of ROWS rows with NW wavefronts, HBM -> LDS without registers: one instruction fills 1 KiB, lane l its bytes
 // 16 l ..; the lane fetches the chunk whose slot that is.
 template <int HD, int ROWS, int NW> struct TileLoad {
     static constexpr int ROW_BYTES = 2 * HD, RPI = 1024 / ROW_BYTES, PASSES = ROWS / (RPI * NW);
-    static_assert(ROWS % (RPI * NW) == 0 && (RPI * NW) % 16 == 0, "every pass covers the same rows of the swizzle");
+    static_assert(ROWS % (RPI * NW) == 0, "whole passes");
     uint32_t voff;
     int row, chunk, wave;
     __device__ __forceinline__ void init(int64_t stride, int w)
@@ -113,11 +130,11 @@ template <int HD, int ROWS, int NW> struct TileLoad {
     {
         if (rows >= ROWS && nch == HD / 8) {
 #pragma unroll
-            for (int i = 0; i < PASSES; ++i, base += RPI * NW * stride) dma16(base, voff, lds + (wave + NW * i) * 1024);
+            for (int i = 0; i < PASSES; ++i, base += RPI * NW * stride) dma16(base, voff, lds + (wave + NW * i) * 1040);
         } else {
 #pragma unroll
             for (int i = 0; i < PASSES; ++i, base += RPI * NW * stride) {
-                char *const dst = lds + (wave + NW * i) * 1024;
+                char *const dst = lds + (wave + NW * i) * 1040;
                 if (row + RPI * NW * i < rows && chunk < nch) dma16(base, voff, dst);
                 else *reinterpret_cast<uint4 *>(dst + (threadIdx.x & 63) * 16) = make_uint4(0, 0, 0, 0);
             }
@@ -132,26 +149,37 @@ __device__ __forceinline__ void dma16_at(const char *src, const char *lds)
     asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(lds_base));
 }
 
-// What this wavefront has requested has landed, and so has everyone else's; nothing is moved across.
+// What this wavefront has requested has landed, and so has everyone else's; nothing is moved across.  (The wait as a builtin: the
+// compiler then knows that its own loads have landed too.  It would otherwise wait for them again at their first use in a loop,
+// by a count that takes in the loads into LDS that it does not know of.)
 __device__ __forceinline__ void landed()
 {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
 }
 
+// (Lane addresses are a base and an XOR with what the compiler knows.  Kept for a whole loop they would be eight registers a tile:
+// fresh() hides the base's origin, so that they are made again where they are used.)
 // Operand of 32 rows of a tile, reduction along them (16 columns from 16 kk): lane l has row base + l % 32, columns 16 kk + 8 (l / 32) ..
+// `offset`: bytes from the operand's own tile, a constant.
 template <int HD, class T> struct RowOperand {
     const char *at;
     int f;
     __device__ __forceinline__ RowOperand(const char *lds)
     {
         const int l = threadIdx.x & 63;
-        at = lds + (l & 31) * (2 * HD);
+        at = lds + row_at<HD>(l & 31);
         f = (swz_a<HD>(l & 31) ^ (l >> 5)) << 4;
     }
-    __device__ __forceinline__ typename In<T>::vec get(int base, int kk) const
+    __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(f)); }
+    __device__ __forceinline__ typename In<T>::vec get(int offset, int kk) const
     {
-        return *reinterpret_cast<const typename In<T>::vec *>(at + (f ^ (kk << 5)) + base * (2 * HD));
+        // (of the bits that the XOR leaves alone the address is a sum)
+        constexpr int PLAIN = HD >= 128 ? 32 : 0;
+        return *reinterpret_cast<const typename In<T>::vec *>(at + (f ^ ((kk << 5) & ~PLAIN)) + ((kk << 5) & PLAIN) + offset);
     }
 };
 
@@ -159,20 +187,21 @@ template <int HD, class T> struct RowOperand {
 // are rows 16 ks + 4 (l / 32) + {0 .. 3, 8 .. 11}: the order in which a 32 x 32 result lies in a lane's registers, so that such a
 // result is the other operand as it is.
 template <int HD, class T> struct ColOperand {
-    const char *lo;
-    int fl, fh;
+    const char *at;
+    int f;
     __device__ __forceinline__ ColOperand(const char *lds)
     {
         const int l = threadIdx.x & 63, r = 4 * (l >> 5) + ((l & 15) >> 2), chunk = 2 * ((l >> 4) & 1) + ((l & 3) >> 1);
-        lo = lds + r * (2 * HD) + ((l & 1) << 3);
-        fl = (chunk ^ swz_a<HD>(r)) << 4;
-        fh = (chunk ^ swz_a<HD>(r + 8)) << 4;
+        at = lds + row_at<HD>(r) + ((l & 1) << 3);
+        f = (chunk ^ swz_a<HD>(r)) << 4;
     }
-    __device__ __forceinline__ typename In<T>::vec get(int db, int ks) const
+    __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(f)); }
+    __device__ __forceinline__ typename In<T>::vec get(int offset, int db, int ks) const
     {
-        const char *const p = lo + ks * 16 * (2 * HD);
-        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + (fl ^ (db << 6))));
-        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + 8 * (2 * HD) + (fh ^ (db << 6))));
+        static_assert(swz_a<HD>(8) == swz_a<HD>(0) && swz_a<HD>(16) == swz_a<HD>(0), "the same for every eight rows");
+        const char *const p = at + (f ^ (db << 6)) + row_at<HD>(16) * ks + offset;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)p);
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + row_at<HD>(8)));
         return __builtin_bit_cast(typename In<T>::vec, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 };

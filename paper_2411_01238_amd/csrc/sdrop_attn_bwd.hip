@@ -14,14 +14,16 @@ namespace sdrop {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-// dV's P is held as 256 P: over thousands of keys P itself would fall among fp16's smallest numbers, whose steps are coarse.  (The
-// factor is part of lse and delta and leaves dS as it is.)
+// Statistics of the rows, two floats each: (lse log2(e) - kPShift, delta kPScale).  dV's P is held as 256 P: over thousands of keys P
+// itself would fall among fp16's smallest numbers, whose steps are coarse.  The factor is part of the two and leaves dS as it is.
 constexpr float kPShift = 8.f, kPScale = 1.f / 256.f;
 
-// Row r of (sequence b, key head hkv): its place among all rows' statistics.
+// Where the rows of (sequence b, key head hkv) begin in them: on 16 bytes, sequences and heads apart.  A tile of 64 rows is read
+// whole, so the array is that much longer than its last row.
 __device__ __forceinline__ int64_t stats_at(const AttnParams &P, const Sequence &s, int b, int hkv)
 {
-    return P.cu_q ? (s.q0 * P.Hkv + (int64_t)hkv * s.Lq) * P.G : ((int64_t)b * P.Hkv + hkv) * P.max_rows;
+    return P.cu_q ? hkv * ((P.total_q * P.G + 2 * P.B + 1) & ~int64_t(1)) + ((s.q0 * P.G + 2 * b) & ~int64_t(1))
+                  : ((int64_t)b * P.Hkv + hkv) * ((P.max_rows + 1) & ~1);
 }
 
 template <class T> __device__ __forceinline__ float dot8(uint4 a, uint4 b, float sum)
@@ -35,24 +37,26 @@ template <class T> __device__ __forceinline__ float dot8(uint4 a, uint4 b, float
 
 // dQ.  As in the forward pass a lane holds keys of one query: S^T = K Q^T, dP^T = V dO^T, dQ^T = K^T dS^T; lse and delta are one number
 // per lane each.
-template <class T, int HD>
+// QW wavefronts own rows of their own; the 4 / QW wavefronts of the same rows take a tile's blocks of 32 keys in turn and are joined at
+// the end.
+template <class T, int HD, int QW>
 __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams P)
 {
-    constexpr int TKV = 64, TILE = TKV * HD * 2, DB = HD / 32;
+    constexpr int TKV = 64, TILE = tile_bytes<HD>(TKV), DB = HD / 32, KW = 4 / QW, ROWS = 32 * QW;
     __shared__ __attribute__((aligned(1024))) char lds[4 * TILE];
-    const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), h = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), h = lane >> 5, wq = wave % QW, wk = wave / QW;
     int bh, unit;
     place(P, P.tiles, bh, unit);
     const int b = bh / P.Hkv, hkv = bh - b * P.Hkv, tile = P.tiles - 1 - unit;
     const Sequence s = sequence_of(P, b);
     if (!s.ok) return;
-    const int rows = s.Lq * P.G, R0 = tile * 128;
+    const int rows = s.Lq * P.G, R0 = tile * ROWS;
     if (R0 >= rows) return;
-    const int off = s.Lk - s.Lq, r_last = min(R0 + 128, rows) - 1;
+    const int off = s.Lk - s.Lq, r_last = min(R0 + ROWS, rows) - 1;
     const int k_end = P.causal ? min(s.Lk, token_of(P, r_last) + off + 1) : s.Lk;
     const int n_tiles = k_end > 0 ? (k_end + TKV - 1) / TKV : 0;
 
-    const int w0 = R0 + 32 * wave, r = w0 + (lane & 31);
+    const int w0 = R0 + 32 * wq, r = w0 + (lane & 31);
     const bool live = r < rows;
     const int i = token_of(P, min(r, rows - 1)), head = hkv * P.G + (min(r, rows - 1) - i * P.G);
     const int lim = !live ? -1 : P.causal ? min(s.Lk - 1, i + off) : s.Lk - 1;
@@ -86,7 +90,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams P)
     if (live) {
         const float x = P.lse[P.cu_q ? head * P.total_q + s.q0 + i : ((int64_t)b * P.Hq + head) * P.max_q + i];
         if (x != -INFINITY) lse2 = x * kLog2e;
-        if (h == 0) reinterpret_cast<float2 *>(P.delta)[stats_at(P, s, b, hkv) + r] = make_float2(lse2, delta);
+        if (h == 0 && wk == 0) reinterpret_cast<float2 *>(P.delta)[stats_at(P, s, b, hkv) + r] = make_float2(lse2 - kPShift, delta * kPScale);
     }
 
     f32x16 acc[DB];
@@ -114,11 +118,9 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams P)
         if (P.causal && kv0 > w_last) continue;
         const char *const kt = lds + buf * 2 * TILE, *const vt = kt + TILE;
         const bool masked = kv0 + TKV > s.Lk || (P.causal && kv0 + TKV - 1 > w_first);
-        // (one block of 32 keys after the other: the registers of two do not fit beside Q, dO and dQ)
-#pragma unroll 1
-        for (int mb = 0; mb < 2; ++mb) {
-            const RowOperand<HD, T> ka(kt + mb * 64 * HD), va(vt + mb * 64 * HD);
-            const ColOperand<HD, T> kc(kt + mb * 64 * HD);
+        auto block = [&](int mb) __attribute__((always_inline)) {
+            const RowOperand<HD, T> ka(kt + mb * row_at<HD>(32)), va(vt + mb * row_at<HD>(32));
+            const ColOperand<HD, T> kc(kt + mb * row_at<HD>(32));
             f32x16 sc = zero16(), dp = zero16();
 #pragma unroll
             for (int kk = 0; kk < HD / 16; ++kk) sc = In<T>::mfma(ka.get(0, kk), qf[kk], sc);
@@ -136,9 +138,33 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams P)
             for (int ks = 0; ks < 2; ++ks) {
                 const typename In<T>::vec ds = narrow8<T>(sc, ks);
 #pragma unroll
-                for (int d = 0; d < DB; ++d) acc[d] = In<T>::mfma(kc.get(d, ks), ds, acc[d]);
+                for (int d = 0; d < DB; ++d) acc[d] = In<T>::mfma(kc.get(0, d, ks), ds, acc[d]);
             }
+        };
+        // (one block of 32 keys after the other: the registers of two do not fit beside Q, dO and dQ)
+        if constexpr (KW == 2) {
+            block(wk);
+        } else {
+#pragma unroll 1
+            for (int mb = 0; mb < 2; ++mb) block(mb);
         }
+    }
+    if constexpr (KW == 2) {
+        float *const joined = reinterpret_cast<float *>(lds) + wq * DB * 16 * 64 + lane;
+        static_assert(QW * DB * 16 * 64 * 4 <= 4 * TILE, "room for the accumulators of half of the wavefronts");
+        landed();
+        if (wk == 1) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) joined[(d * 16 + e) * 64] = acc[d][e];
+        }
+        __syncthreads();
+        if (wk == 1) return;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[d][e] += joined[(d * 16 + e) * 64];
     }
     char *const dst = P.dq + (P.cu_q ? 0 : b * P.dq_b) + (s.q0 + i) * P.dq_t + head * P.dq_h;
 #pragma unroll
@@ -146,17 +172,18 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams P)
 }
 
 // dK and dV.  A wavefront owns 32 keys; a lane holds rows (queries) of one key: S = Q K^T, dP = dO V^T, dV^T = dO^T P, dK^T = Q^T dS.
-template <class T, int HD>
-__global__ __launch_bounds__(256, HD <= 64 ? 2 : 1) void attn_dkv_kernel(AttnParams P)
+// KW wavefronts own keys of their own; the 4 / KW wavefronts of the same keys take a tile's blocks of 32 rows in turn and are joined at
+// the end.
+template <class T, int HD, int KW>
+__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnParams P)
 {
-    constexpr int TQ = 64, TILE = TQ * HD * 2, DB = HD / 32;
-    __shared__ __attribute__((aligned(1024))) char lds[4 * TILE];
-    __shared__ float st_lse[2][TQ], st_delta[2][TQ];
-    __shared__ int st_lim[2][TQ];                   // last key that the row sees
+    constexpr int TQ = 64, TILE = tile_bytes<HD>(TQ), DB = HD / 32, RW = 4 / KW, KEYS = 32 * KW;
+    __shared__ __attribute__((aligned(1024))) char lds[4 * TILE + 2 * TQ * 8];
+    float *const st = reinterpret_cast<float *>(lds + 4 * TILE);       // [2][TQ][2]
     const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), h = lane >> 5;
     int bh, unit;
     place(P, P.tiles, bh, unit);
-    const int b = bh / P.Hkv, hkv = bh - b * P.Hkv, K0 = unit * 128;
+    const int b = bh / P.Hkv, hkv = bh - b * P.Hkv, K0 = unit * KEYS, wk = wave % KW, wr = wave / KW;
     const Sequence s = sequence_of(P, b);
     if (!s.ok) return;
     // rows of dK and dV that this call writes; behind a dense sequence's last key they are 0
@@ -167,8 +194,9 @@ __global__ __launch_bounds__(256, HD <= 64 ? 2 : 1) void attn_dkv_kernel(AttnPar
     const int r_first = P.causal ? min(max(K0 - off, 0), s.Lq) * P.G : 0;
     const int t0 = r_first / TQ, t1 = (rows + TQ - 1) / TQ;
 
-    const int w0 = K0 + 32 * wave, key = w0 + (lane & 31);
+    const int w0 = K0 + 32 * wk, key = w0 + (lane & 31);
     const bool live = key < s.Lk;
+    const int first_row = (int)max((int64_t)-1, min((int64_t)(key - off) * P.G, (int64_t)INT_MAX));      // causal: of those that see the key
     typename In<T>::vec kf[HD / 16], vf[HD / 16];
     {
         const int64_t at = s.k0 + min(key, max(s.Lk - 1, 0));
@@ -192,104 +220,146 @@ __global__ __launch_bounds__(256, HD <= 64 ? 2 : 1) void attn_dkv_kernel(AttnPar
 
     const char *const qb = P.q + (P.cu_q ? 0 : b * P.q_b) + s.q0 * P.q_t + (int64_t)hkv * P.G * P.q_h;
     const char *const gb = P.dout + (P.cu_q ? 0 : b * P.do_b) + s.q0 * P.do_t + (int64_t)hkv * P.G * P.do_h;
-    const float2 *const stats = reinterpret_cast<const float2 *>(P.delta) + stats_at(P, s, b, hkv);
+    const char *const stats = reinterpret_cast<const char *>(reinterpret_cast<const float2 *>(P.delta) + stats_at(P, s, b, hkv));
     const int nch = P.D / 8;
     // rows of a tile are tokens and heads of the group in turn: each lane works out where its rows lie
     constexpr int ROW_BYTES = 2 * HD, RPI = 1024 / ROW_BYTES, PASSES = TQ / (RPI * 4);
-    const int lrow = RPI * wave + (lane * 16) / ROW_BYTES, chunk = ((lane * 16) % ROW_BYTES >> 4) ^ swz_a<HD>(lrow);
     auto request = [&](int t, int buf) __attribute__((always_inline)) {
+        // (made anew for every tile: kept over the loop they are registers that the accumulators need)
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        const int lrow = RPI * wave + (ln * 16) / ROW_BYTES, chunk = ((ln * 16) % ROW_BYTES >> 4) ^ swz_a<HD>(lrow);
         char *const dst = lds + buf * 2 * TILE;
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             const int rr = t * TQ + lrow + RPI * 4 * p;
-            char *const at = dst + (wave + 4 * p) * 1024;
+            char *const at = dst + (wave + 4 * p) * 1040;
             if (rr < rows && chunk < nch) {
                 const int tok = token_of(P, rr), g = rr - tok * P.G;
                 dma16_at(qb + tok * P.q_t + g * P.q_h + chunk * 16, at);
                 dma16_at(gb + tok * P.do_t + g * P.do_h + chunk * 16, at + TILE);
             } else {
-                *reinterpret_cast<uint4 *>(at + lane * 16) = make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4 *>(at + TILE + lane * 16) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>(at + ln * 16) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4 *>(at + TILE + ln * 16) = make_uint4(0, 0, 0, 0);
             }
         }
+        if (threadIdx.x < TQ / 2) dma16_at(stats + (int64_t)t * TQ * 8 + ln * 16, lds + 4 * TILE + buf * TQ * 8);
     };
-    // A tile's statistics go through a register: asked for with the tile, put into LDS when the tile before it has been computed
-    // (the compiler's own wait for them would otherwise be one for the whole tile).
-    float2 next = make_float2(INFINITY, 0.f);
-    auto ask = [&](int t) __attribute__((always_inline)) {
-        const int rr = t * TQ + (int)threadIdx.x;
-        next = threadIdx.x < TQ && rr < rows ? stats[rr] : make_float2(INFINITY, 0.f);
-    };
-    auto put = [&](int t, int buf) __attribute__((always_inline)) {
-        if (threadIdx.x < TQ) {
-            const int rr = t * TQ + (int)threadIdx.x;
-            st_lse[buf][threadIdx.x] = next.x - kPShift;
-            st_delta[buf][threadIdx.x] = next.y * kPScale;
-            st_lim[buf][threadIdx.x] = rr < rows ? token_of(P, rr) + off : -1;
-        }
-    };
-    if (t0 < t1) {
-        ask(t0);
-        request(t0, 0);
-        put(t0, 0);
-    }
+    if (t0 < t1) request(t0, 0);
     for (int t = t0; t < t1; ++t) {
         const int buf = (t - t0) & 1;
         landed();
-        if (t + 1 < t1) {
-            ask(t + 1);
-            request(t + 1, buf ^ 1);
-        }
-        const char *const qt = lds + buf * 2 * TILE, *const gt = qt + TILE;
-        const RowOperand<HD, T> qa(qt), ga(gt);
-        const ColOperand<HD, T> qc(qt), gc(gt);
-#pragma unroll
-        for (int mb = 0; mb < 2; ++mb) {
+        if (t + 1 < t1) request(t + 1, buf ^ 1);
+        auto block = [&](int mb) __attribute__((always_inline)) {
             const int rb = t * TQ + 32 * mb;
-            if (rb >= rows) continue;
+            if (rb >= rows) return;
             const int see_first = P.causal ? uni(token_of(P, rb)) + off : s.Lk, see_last = P.causal ? uni(token_of(P, min(rb + 31, rows - 1))) + off : s.Lk;
-            if (see_last < w0) continue;            // none of these rows sees a key of this wavefront
+            if (see_last < w0) return;            // none of these rows sees a key of this wavefront
+            RowOperand<HD, T> ra(lds + buf * 2 * TILE + mb * row_at<HD>(32));
+            ColOperand<HD, T> ca(lds + buf * 2 * TILE + mb * row_at<HD>(32));
+            ra.fresh();
+            ca.fresh();
             f32x16 sc = zero16(), dp = zero16();
 #pragma unroll
-            for (int kk = 0; kk < HD / 16; ++kk) sc = In<T>::mfma(qa.get(32 * mb, kk), kf[kk], sc);
+            for (int kk = 0; kk < HD / 16; ++kk) sc = In<T>::mfma(ra.get(0, kk), kf[kk], sc);
 #pragma unroll
-            for (int kk = 0; kk < HD / 16; ++kk) dp = In<T>::mfma(ga.get(32 * mb, kk), vf[kk], dp);
-            if (P.causal && see_first < w0 + 31) {
+            for (int kk = 0; kk < HD / 16; ++kk) dp = In<T>::mfma(ra.get(TILE, kk), vf[kk], dp);
+            const float *const stb = st + (buf * TQ + 32 * mb + 4 * h) * 2;
+            // the operands are read two ahead of the matrix instructions (three would not leave the accumulators their registers)
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
 #pragma unroll
-                for (int g = 0; g < 4; ++g)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (key > st_lim[buf][32 * mb + 8 * g + 4 * h + e]) sc[4 * g + e] = -INFINITY;
+            for (int i = 0; i < HD / 8 - 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             }
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32q l4 = *reinterpret_cast<const f32q *>(&st_lse[buf][32 * mb + 8 * g + 4 * h]);
-                const f32q d4 = *reinterpret_cast<const f32q *>(&st_delta[buf][32 * mb + 8 * g + 4 * h]);
+                const f32q a4 = *reinterpret_cast<const f32q *>(stb + 16 * g), b4 = *reinterpret_cast<const f32q *>(stb + 16 * g + 4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(sc[4 * g + e] * P.c - l4[e]);
+                    const float p = __builtin_amdgcn_exp2f(sc[4 * g + e] * P.c - (e < 2 ? a4 : b4)[2 * (e & 1)]);
                     sc[4 * g + e] = p;
-                    dp[4 * g + e] = p * (dp[4 * g + e] * kPScale - d4[e]);
+                    dp[4 * g + e] = p * (dp[4 * g + e] * kPScale - (e < 2 ? a4 : b4)[2 * (e & 1) + 1]);
                 }
             }
+            // rows that do not see the key, and rows that do not exist (whose statistics are another's, or none)
+            if ((P.causal && see_first < w0 + 31) || rb + 32 > rows) {
+                const int from = (P.causal ? first_row : 0) - rb - 4 * h, to = rows - rb - 4 * h;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int at = 8 * (e >> 2) + (e & 3);
+                    if (at < from || at >= to) sc[e] = dp[e] = 0.f;
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            typename In<T>::vec pn[2], dn[2];
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) { pn[ks] = narrow8<T>(sc, ks); dn[ks] = narrow8<T>(dp, ks); }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
-                const typename In<T>::vec p = narrow8<T>(sc, ks), ds = narrow8<T>(dp, ks);
+                const typename In<T>::vec p = pn[ks], ds = dn[ks];
 #pragma unroll
-                for (int d = 0; d < DB; ++d) dv[d] = In<T>::mfma(gc.get(d, 2 * mb + ks), p, dv[d]);
+                for (int d = 0; d < DB; ++d) dv[d] = In<T>::mfma(ca.get(TILE, d, ks), p, dv[d]);
 #pragma unroll
-                for (int d = 0; d < DB; ++d) dk[d] = In<T>::mfma(qc.get(d, 2 * mb + ks), ds, dk[d]);
+                for (int d = 0; d < DB; ++d) dk[d] = In<T>::mfma(ca.get(0, d, ks), ds, dk[d]);
             }
+            // two operands ahead
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int i = 0; i < 4 * DB - 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        if constexpr (RW == 2) {
+            block(wr);
+        } else {
+            // (one block of 32 rows after the other: the registers of two do not fit beside K, V, dK and dV)
+#pragma unroll 1
+            for (int mb = 0; mb < 2; ++mb) block(mb);
         }
-        if (t + 1 < t1) put(t + 1, buf ^ 1);
     }
-    if (!live) {
+    if constexpr (RW == 2) {
+        static_assert(2 * KW * DB * 16 * 64 * 4 <= 4 * TILE, "room for the accumulators of half of the wavefronts");
+        int ln = lane;
+        asm volatile("" : "+v"(ln));
+        float *const joined = reinterpret_cast<float *>(lds) + wk * 2 * DB * 16 * 64 + ln;
+        landed();
+        if (wr == 1) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    joined[(d * 16 + e) * 64] = dk[d][e];
+                    joined[((DB + d) * 16 + e) * 64] = dv[d][e];
+                }
+        }
+        __syncthreads();
+        if (wr == 1) return;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                dk[d][e] += joined[(d * 16 + e) * 64];
+                dv[d][e] += joined[((DB + d) * 16 + e) * 64];
+            }
+    }
+    // (made again, as in request)
+    int mine = lane & 31;
+    asm volatile("" : "+v"(mine));
+    mine += w0;
+    if (mine >= s.Lk) {
 #pragma unroll
         for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zero16();
     }
-    const bool write = key < out_rows;
-    char *const dkp = P.dk + (P.cu_k ? 0 : b * P.dk_b) + (s.k0 + key) * P.dk_t + hkv * P.dk_h;
-    char *const dvp = P.dv + (P.cu_k ? 0 : b * P.dv_b) + (s.k0 + key) * P.dv_t + hkv * P.dv_h;
+    const bool write = mine < out_rows;
+    char *const dkp = P.dk + (P.cu_k ? 0 : b * P.dk_b) + (s.k0 + mine) * P.dk_t + hkv * P.dk_h;
+    char *const dvp = P.dv + (P.cu_k ? 0 : b * P.dv_b) + (s.k0 + mine) * P.dv_t + hkv * P.dv_h;
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
         store_row32<T>(dkp + 64 * d, dk[d], P.scale, P.D - 32 * d, write);
@@ -297,20 +367,47 @@ __global__ __launch_bounds__(256, HD <= 64 ? 2 : 1) void attn_dkv_kernel(AttnPar
     }
 }
 
+// dK and dV on tiles of 64 keys, two wavefronts sharing out the rows of the same keys, instead of 128: where the larger tiles leave the
+// chip half empty, or where they are all at work at once and the longest of them (the first keys under a causal mask, the longest of
+// packed sequences) is what the call waits for.  Small tiles read each row twice as often.  us, 128 -> 64: 4096 tokens, 8 heads of
+// 128, no mask 210 -> 196, causal 172 -> 125; 2 x 2048, 16 heads of 64, causal 68 -> 55; but 2 x 4096, 16 heads of 128, causal 349 -> 430;
+// 4 x 1024, 16 heads of 128, causal 60 -> 66; 32 x 128, 8 heads of 128, causal 14.0 -> 15.4.
+bool few_key_tiles(const AttnParams &P)
+{
+    const int64_t keys = P.cu_k ? P.total_k : (int64_t)P.B * P.max_k, tiles = keys / 128 * P.Hkv;
+    return P.max_k >= 1024 && tiles <= (P.causal || P.cu_k ? 2 : 1) * (int64_t)cu_count() && !(P.causal && !P.cu_k && P.max_k < 2048 && tiles > cu_count());
+}
+
+// dQ on 64 rows a workgroup, two wavefronts sharing out the keys of the same rows, instead of 128.  us, 128 -> 64: 2048 tokens, 8
+// heads of 128, no mask 65 -> 44, causal 62 -> 40; 4096 tokens, causal 121 -> 86; heads of 64: 2 x 2048, 16 heads, causal 53 -> 44, 4 x 2048
+// 95 -> 77, 2 x 4096, no mask 271 -> 252; but 2 x 4096, 16 heads of 128 257 -> 282, 32 x 128, 8 heads of 128 18.5 -> 20.0.
+bool few_rows(const AttnParams &P)
+{
+    return (P.max_k >= 512 && (int64_t)P.B * P.Hkv * ((P.max_rows + 127) / 128) <= cu_count()) || (P.D <= 64 && P.max_k >= 2048);
+}
+
 template <class T, int HD> int launch_bwd(AttnParams P, hipStream_t st)
 {
-    P.tiles = (P.max_rows + 127) / 128;
-    hipLaunchKernelGGL((attn_dq_kernel<T, HD>), dim3((unsigned)((int64_t)P.B * P.Hkv * P.tiles)), dim3(256), 0, st, P);
+    const int rows = few_rows(P) ? 64 : 128;
+    P.tiles = (P.max_rows + rows - 1) / rows;
+    const dim3 row_grid((unsigned)((int64_t)P.B * P.Hkv * P.tiles));
+    if (rows == 64) hipLaunchKernelGGL((attn_dq_kernel<T, HD, 2>), row_grid, dim3(256), 0, st, P);
+    else hipLaunchKernelGGL((attn_dq_kernel<T, HD, 4>), row_grid, dim3(256), 0, st, P);
     const int rc = hip_status(hipGetLastError());
     if (rc != SDROP_OK) return rc;
-    P.tiles = (P.max_k + 127) / 128;
-    hipLaunchKernelGGL((attn_dkv_kernel<T, HD>), dim3((unsigned)((int64_t)P.B * P.Hkv * P.tiles)), dim3(256), 0, st, P);
+    const bool few = few_key_tiles(P);
+    const int keys = few ? 64 : 128;
+    P.tiles = (P.max_k + keys - 1) / keys;
+    const dim3 grid((unsigned)((int64_t)P.B * P.Hkv * P.tiles));
+    if (few) hipLaunchKernelGGL((attn_dkv_kernel<T, HD, 2>), grid, dim3(256), 0, st, P);
+    else hipLaunchKernelGGL((attn_dkv_kernel<T, HD, 4>), grid, dim3(256), 0, st, P);
     return hip_status(hipGetLastError());
 }
 
 size_t stats_bytes(const AttnParams &P)
 {
-    return (P.cu_q ? (size_t)P.total_q * P.Hq : (size_t)P.B * P.Hkv * P.max_rows) * 2 * sizeof(float);
+    const size_t rows = P.cu_q ? (size_t)P.Hkv * (((size_t)P.total_q * P.G + 2 * P.B + 1) & ~size_t(1)) : (size_t)P.B * P.Hkv * ((P.max_rows + 1) & ~1);
+    return (rows + 64) * 2 * sizeof(float);
 }
 
 }  // namespace
@@ -337,7 +434,7 @@ int sdrop_attn_bwd(const void *dO, const void *q, const void *k, const void *v, 
         !aligned16(dv) || reinterpret_cast<uintptr_t>(lse) % 4) return SDROP_EALIGN;
     if (!ws || ws_bytes < stats_bytes(P) || !aligned16(ws)) return SDROP_EWORKSPACE;
     const int64_t most = (int64_t(1) << 24) - 1, heads = (int64_t)P.B * P.Hkv;      // (a launch counts its threads in 32 bits)
-    if (heads * ((P.max_rows + 127) / 128) > most || heads * (((int64_t)P.max_k + 127) / 128) > most) return SDROP_ESHAPE;
+    if (heads * (((int64_t)P.max_rows + 63) / 64) > most || heads * (((int64_t)P.max_k + 63) / 64) > most) return SDROP_ESHAPE;
     P.dout = static_cast<const char *>(dO);
     P.q = static_cast<const char *>(q);
     P.k = static_cast<const char *>(k);

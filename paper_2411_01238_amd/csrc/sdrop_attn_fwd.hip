@@ -12,13 +12,13 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// QW: wavefronts of the workgroup that own rows of their own (32 each); the 4 / QW wavefronts of the same rows take the keys of a tile in
-// turn and are joined at the end.  MB: blocks of 32 keys per wavefront and tile.
-template <class T, int HD, int QW, int MB>
-__global__ __launch_bounds__(256, QW == 1 && HD > 64 ? 1 : 2) void attn_fwd_kernel(AttnParams P)
+// QW: wavefronts of the workgroup that own rows of their own (32 each); KW (1 or 2) wavefronts of the same rows take the keys of a tile in
+// turn and are joined at the end.  MB: blocks of 32 keys per wavefront and tile.  STAGES: tiles that LDS holds.
+template <class T, int HD, int QW, int KW, int MB, int STAGES>
+__global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? 2 : 1) void attn_fwd_kernel(AttnParams P)
 {
-    constexpr int KW = 4 / QW, TKV = 32 * MB * KW, TILE = TKV * HD * 2, DB = HD / 32;
-    __shared__ __attribute__((aligned(1024))) char lds[4 * TILE];
+    constexpr int TKV = 32 * MB * KW, TILE = tile_bytes<HD>(TKV), DB = HD / 32;
+    __shared__ __attribute__((aligned(1024))) char lds[STAGES * 2 * TILE];
     const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), wq = wave % QW, wk = wave / QW, h = lane >> 5;
 
     int bh, unit;
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256, QW == 1 && HD > 64 ? 1 : 2) void attn_fwd_kern
     const int w_first = any ? uni(token_of(P, w0)) + off : 0, w_last = any ? uni(token_of(P, min(w0 + 31, rows - 1))) + off : -1;
 
     typename In<T>::vec qf[HD / 16];
-    {
+    auto load_q = [&]() __attribute__((always_inline)) {
         const char *const qp = P.q + (P.cu_q ? 0 : b * P.q_b) + (s.q0 + i) * P.q_t + head * P.q_h;
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) {
@@ -54,42 +54,22 @@ __global__ __launch_bounds__(256, QW == 1 && HD > 64 ? 1 : 2) void attn_fwd_kern
             if (live && col < P.D) x = *reinterpret_cast<const uint4 *>(qp + 2 * col);
             qf[kk] = __builtin_bit_cast(typename In<T>::vec, x);
         }
-    }
+    };
 
     f32x16 o[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = zero16();
     float m = -INFINITY, l = 0.f;           // running maximum (of S before the scale) and this lane's part of the sum
 
-    const char *kb = P.k + (P.cu_k ? 0 : b * P.k_b) + s.k0 * P.k_t + hkv * P.k_h + (int64_t)t0 * TKV * P.k_t;
-    const char *vb = P.v + (P.cu_k ? 0 : b * P.v_b) + s.k0 * P.v_t + hkv * P.v_h + (int64_t)t0 * TKV * P.v_t;
-    const int nch = P.D / 8;
-    TileLoad<HD, TKV, 4> lk, lv;
-    lk.init(P.k_t, wave);
-    lv.init(P.v_t, wave);
-    auto request = [&](int t, int buf) __attribute__((always_inline)) {
-        const int left = s.Lk - t * TKV;
-        lk.issue(kb, P.k_t, lds + buf * 2 * TILE, left, nch);
-        lv.issue(vb, P.v_t, lds + buf * 2 * TILE + TILE, left, nch);
-        kb += TKV * P.k_t;
-        vb += TKV * P.v_t;
-    };
-    if (t0 < t1) request(t0, 0);
-    for (int t = t0; t < t1; ++t) {
-        const int buf = (t - t0) & 1;
-        landed();
-        if (t + 1 < t1) request(t + 1, buf ^ 1);
-        const int kv0 = t * TKV + wk * 32 * MB;
-        if (kv0 >= s.Lk || (P.causal && kv0 > w_last)) continue;       // (nothing for these rows)
-        const char *const kt = lds + buf * 2 * TILE + wk * 32 * MB * HD * 2, *const vt = kt + TILE;
-
+    // 32 * MB keys from kv0 on, whose K and V lie at kt and vt
+    auto compute_keys = [&](int kv0, const char *kt, const char *vt) __attribute__((always_inline)) {
         f32x16 sc[MB];
         const RowOperand<HD, T> ka(kt);
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
             sc[mb] = zero16();
 #pragma unroll
-            for (int kk = 0; kk < HD / 16; ++kk) sc[mb] = In<T>::mfma(ka.get(32 * mb, kk), qf[kk], sc[mb]);
+            for (int kk = 0; kk < HD / 16; ++kk) sc[mb] = In<T>::mfma(ka.get(row_at<HD>(32) * mb, kk), qf[kk], sc[mb]);
         }
         if (kv0 + 32 * MB > s.Lk || (P.causal && kv0 + 32 * MB - 1 > w_first)) {
             const int last = lim - kv0 - 4 * h;
@@ -129,56 +109,110 @@ __global__ __launch_bounds__(256, QW == 1 && HD > 64 ? 1 : 2) void attn_fwd_kern
         for (int ks = 0; ks < 2 * MB; ++ks) {
             const typename In<T>::vec p = narrow8<T>(sc[ks >> 1], ks & 1);
 #pragma unroll
-            for (int d = 0; d < DB; ++d) o[d] = In<T>::mfma(va.get(d, ks), p, o[d]);
+            for (int d = 0; d < DB; ++d) o[d] = In<T>::mfma(va.get(0, d, ks), p, o[d]);
+        }
+    };
+
+    const int kv_first = t0 * TKV, nch = P.D / 8;
+    if constexpr (QW > 1) {
+        const char *kb = P.k + (P.cu_k ? 0 : b * P.k_b) + (s.k0 + kv_first) * P.k_t + hkv * P.k_h;
+        const char *vb = P.v + (P.cu_k ? 0 : b * P.v_b) + (s.k0 + kv_first) * P.v_t + hkv * P.v_h;
+        TileLoad<HD, TKV, 4> lk, lv;
+        lk.init(P.k_t, wave);
+        lv.init(P.v_t, wave);
+        auto request = [&](int t, int buf) __attribute__((always_inline)) {
+            const int left = s.Lk - t * TKV;
+            lk.issue(kb, P.k_t, lds + buf * 2 * TILE, left, nch);
+            lv.issue(vb, P.v_t, lds + buf * 2 * TILE + TILE, left, nch);
+            kb += TKV * P.k_t;
+            vb += TKV * P.v_t;
+        };
+        load_q();
+        if (t0 < t1) request(t0, 0);
+        for (int t = t0; t < t1; ++t) {
+            const int buf = (t - t0) & 1;
+            landed();
+            if (t + 1 < t1) request(t + 1, buf ^ 1);
+            const int kv0 = t * TKV + 32 * MB * wk;
+            if ((KW > 1 && kv0 >= s.Lk) || (P.causal && kv0 > w_last)) continue;        // (nothing for these rows)
+            const char *const kt = lds + buf * 2 * TILE + wk * row_at<HD>(32 * MB);
+            compute_keys(kv0, kt, kt + TILE);
+        }
+    } else {
+        // A wavefront streams its own keys through its own part of LDS, STAGES blocks of 32 ahead and without barriers: few rows
+        // are bound by the memory, which wants as much under way as there is room for.
+        constexpr int BLOCK = tile_bytes<HD>(32), LOADS = 2 * 32 * HD / 512;
+        static_assert(MB == 1 && LOADS * (STAGES - 1) < 64, "blocks of 32 keys; what is under way is counted in six bits");
+        char *const mine = lds + wave * STAGES * 2 * BLOCK;
+        const char *kb = P.k + (P.cu_k ? 0 : b * P.k_b) + (s.k0 + kv_first + 32 * wk) * P.k_t + hkv * P.k_h;
+        const char *vb = P.v + (P.cu_k ? 0 : b * P.v_b) + (s.k0 + kv_first + 32 * wk) * P.v_t + hkv * P.v_h;
+        TileLoad<HD, 32, 1> lk, lv;
+        lk.init(P.k_t, 0);
+        lv.init(P.v_t, 0);
+        const int end = min(k_end, t1 * TKV);
+        auto request = [&](int kv0, int stage) __attribute__((always_inline)) {
+            if (kv0 < end) {
+                lk.issue(kb, P.k_t, mine + stage * 2 * BLOCK, s.Lk - kv0, nch);
+                lv.issue(vb, P.v_t, mine + stage * 2 * BLOCK + BLOCK, s.Lk - kv0, nch);
+            }
+            kb += TKV * P.k_t;
+            vb += TKV * P.v_t;
+        };
+        int kv0 = kv_first + 32 * wk;
+#pragma unroll 1
+        for (int i2 = 0; i2 < STAGES; ++i2) request(kv0 + i2 * TKV, i2);
+        load_q();
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+        for (int stage = 0; kv0 < end; kv0 += TKV) {
+            // the blocks behind this one may still be under way: all of their loads if the last of them is whole
+            const int far = kv0 + (STAGES - 1) * TKV;
+            asm volatile("" ::: "memory");
+            if (far < end && far + 32 <= s.Lk) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(LOADS * (STAGES - 1)));
+            else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            const char *const kt = mine + stage * 2 * BLOCK;
+            compute_keys(kv0, kt, kt + BLOCK);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            request(kv0 + STAGES * TKV, stage);
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
     }
     l = join_halves(l, [](float a, float b2) { return a + b2; });
 
-    // the wavefronts of the same rows: each is scaled to the common maximum, each adds up one block of 32 columns (or two)
-    if constexpr (KW > 1) {
-        float *const ml = reinterpret_cast<float *>(lds);
-        float *const ob = reinterpret_cast<float *>(lds) + 2 * 4 * 64;
-        static_assert((2 * 4 * 64 + 4 * DB * 16 * 64) * 4 <= 4 * TILE, "room for the accumulators of all wavefronts");
+    // the two wavefronts of the same rows, scaled to their common maximum; the first one goes on
+    if constexpr (KW == 2) {
+        float *const ml = reinterpret_cast<float *>(lds) + wq * (2 + DB * 16) * 64 + lane, *const ob = ml + 128;
+        static_assert(QW * (2 + DB * 16) * 64 * 4 <= STAGES * 2 * TILE, "room for half of the wavefronts");
         landed();
-        ml[wave * 64 + lane] = m;
-        ml[256 + wave * 64 + lane] = l;
+        if (wk == 1) {
+            ml[0] = m;
+            ml[64] = l;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) ob[(d * 16 + e) * 64] = o[d][e];
+        }
         __syncthreads();
-        float mn = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < KW; ++w) mn = fmaxf(mn, ml[(w * QW + wq) * 64 + lane]);
-        const float ref = mn == -INFINITY ? 0.f : mn;
-        l = 0.f;
-#pragma unroll
-        for (int w = 0; w < KW; ++w)
-            l += ml[256 + (w * QW + wq) * 64 + lane] * __builtin_amdgcn_exp2f((ml[(w * QW + wq) * 64 + lane] - ref) * P.c);
-        const float f = __builtin_amdgcn_exp2f((m - ref) * P.c);
+        if (wk == 1) return;
+        const float m1 = ml[0], mn = fmaxf(m, m1), ref = mn == -INFINITY ? 0.f : mn;
+        const float f0 = __builtin_amdgcn_exp2f((m - ref) * P.c), f1 = __builtin_amdgcn_exp2f((m1 - ref) * P.c);
+        l = l * f0 + ml[64] * f1;
         m = mn;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) ob[((wave * DB + d) * 16 + e) * 64 + lane] = o[d][e] * f;
-        __syncthreads();
-#pragma unroll
-        for (int d = 0; d < DB; ++d) {
-            if (d % KW != wk) continue;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                float t = 0.f;
-#pragma unroll
-                for (int w = 0; w < KW; ++w) t += ob[(((w * QW + wq) * DB + d) * 16 + e) * 64 + lane];
-                o[d][e] = t;
-            }
-        }
+            for (int e = 0; e < 16; ++e) o[d][e] = o[d][e] * f0 + ob[(d * 16 + e) * 64] * f1;
     }
     const float inv = l > 0.f ? 1.f / l : l == l ? 0.f : l;         // (no key seen: 0; NaN stays NaN)
     const float lse = l > 0.f || l != l ? (m * P.c + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     if (P.splits > 1) {
         const int64_t row = ((int64_t)split * P.B * P.Hkv + bh) * P.max_rows + r;
-        if (live && wk == 0 && h == 0) P.part_lse[row] = lse;
+        if (live && h == 0) P.part_lse[row] = lse;
         float *const dst = P.part_o + row * P.D;
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
-            if (d % KW != wk) continue;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int col = 32 * d + 8 * g + 4 * h;
@@ -188,11 +222,10 @@ __global__ __launch_bounds__(256, QW == 1 && HD > 64 ? 1 : 2) void attn_fwd_kern
         }
         return;
     }
-    if (P.lse && live && wk == 0 && h == 0) P.lse[P.cu_q ? head * P.total_q + s.q0 + i : ((int64_t)b * P.Hq + head) * P.max_q + i] = lse;
+    if (P.lse && live && h == 0) P.lse[P.cu_q ? head * P.total_q + s.q0 + i : ((int64_t)b * P.Hq + head) * P.max_q + i] = lse;
     const int64_t at = (P.cu_q ? 0 : b * P.o_b) + (s.q0 + i) * P.o_t + head * P.o_h;
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-        if (d % KW != wk) continue;
         store_row32<T>(P.out + at + 64 * d, o[d], inv, P.D - 32 * d, live, P.out_rest ? P.out_rest + at + 64 * d : nullptr);
     }
 }
@@ -210,18 +243,39 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams P)
         const Sequence s = sequence_of(P, uni(b));
         if (!s.ok || r >= s.Lq * P.G) continue;
         const int i = token_of(P, r), head = (bh - b * P.Hkv) * P.G + r - i * P.G;
-        float mx = -INFINITY;
-        for (int p = 0; p < P.splits; ++p) mx = fmaxf(mx, P.part_lse[(int64_t)p * n + w]);
+        // a lane has the weights of parts lane and lane + 64; the parts' O are asked for eight at a time
+        float x[2], mx = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int p = lane + 64 * u;
+            x[u] = p < P.splits ? P.part_lse[(int64_t)p * n + w] : -INFINITY;
+            mx = fmaxf(mx, x[u]);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
         const float ref = mx == -INFINITY ? 0.f : mx;
         float sum = 0.f, a0 = 0.f, a1 = 0.f;
-        for (int p = 0; p < P.splits; ++p) {
-            const float x = P.part_lse[(int64_t)p * n + w];
-            const float f = __builtin_amdgcn_exp2f((x - ref) * kLog2e);
-            sum += f;
-            if (2 * lane < P.D) {
-                const float2 v = *reinterpret_cast<const float2 *>(P.part_o + ((int64_t)p * n + w) * P.D + 2 * lane);
-                a0 += f * v.x;
-                a1 += f * v.y;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            x[u] = __builtin_amdgcn_exp2f((x[u] - ref) * kLog2e);
+            sum += x[u];
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
+        const float *const src = P.part_o + w * P.D + 2 * lane;
+        for (int p0 = 0; p0 < P.splits; p0 += 8) {
+            float2 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                v[u] = make_float2(0.f, 0.f);
+                if (p0 + u < P.splits && 2 * lane < P.D) v[u] = *reinterpret_cast<const float2 *>(src + (int64_t)(p0 + u) * n * P.D);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int p = p0 + u;
+                const float f = __shfl(p < 64 ? x[0] : x[1], p & 63, 64);
+                a0 += f * v[u].x;
+                a1 += f * v[u].y;
             }
         }
         const float inv = sum > 0.f ? 1.f / sum : sum == sum ? 0.f : sum;
@@ -239,11 +293,16 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams P)
     }
 }
 
-template <class T, int HD> int launch_fwd(AttnParams P, bool few, hipStream_t st)
+// How the forward pass is laid out: rows per workgroup (32: all of its wavefronts share out the keys of the same rows), row tiles and
+// parts of the keys.
+struct FwdPlan { int rows; int64_t tiles, splits; };
+
+template <class T, int HD> int launch_fwd(AttnParams P, const FwdPlan &p, hipStream_t st)
 {
-    const unsigned grid = (unsigned)((int64_t)P.B * P.Hkv * P.tiles * P.splits);
-    if (few) hipLaunchKernelGGL((attn_fwd_kernel<T, HD, 1, 1>), dim3(grid), dim3(256), 0, st, P);
-    else hipLaunchKernelGGL((attn_fwd_kernel<T, HD, 4, 2>), dim3(grid), dim3(256), 0, st, P);
+    const dim3 grid((unsigned)((int64_t)P.B * P.Hkv * P.tiles * P.splits));
+    if (p.rows == 32) hipLaunchKernelGGL((attn_fwd_kernel<T, HD, 1, 2, 1, HD <= 64 ? 4 : 2>), grid, dim3(128), 0, st, P);
+    else if (p.rows == 64) hipLaunchKernelGGL((attn_fwd_kernel<T, HD, 2, 2, 1, 2>), grid, dim3(256), 0, st, P);
+    else hipLaunchKernelGGL((attn_fwd_kernel<T, HD, 4, 1, 2, 2>), grid, dim3(256), 0, st, P);
     const int rc = hip_status(hipGetLastError());
     if (rc != SDROP_OK || P.splits == 1) return rc;
     const int64_t groups = ((int64_t)P.B * P.Hkv * P.max_rows + 3) / 4;
@@ -251,16 +310,20 @@ template <class T, int HD> int launch_fwd(AttnParams P, bool few, hipStream_t st
     return hip_status(hipGetLastError());
 }
 
-// How the forward pass is laid out: few rows (one block of 32, its keys shared out to the workgroup's wavefronts) or 128 rows a
-// workgroup; in how many parts the keys are taken where that leaves CUs without work.
-struct FwdPlan { bool few; int64_t tiles, splits; };
+// 64 rows a workgroup, two wavefronts sharing out the keys of the same rows, where 128 would leave CUs without work, or with one
+// workgroup each and keys enough to share.  us, 128 (in parts of the keys and joined, where that was the faster) -> 64: 2048 tokens,
+// 8 heads of 128, no mask 41 -> 34, causal 34 -> 32; 4096 tokens, causal 76 -> 67; 2 x 2048, 16 heads of 64, causal 38 -> 32; but
+// 2 x 2048, 16 heads of 128, causal 55 -> 58; 32 x 128, 8 heads of 128, causal 12.1 -> 13.4.
+// Parts of the keys cost a pass over what they leave (12 us for 2048 rows of 8 heads): for few rows they fill the chip twice (16384
+// keys of 16 sequences, 8 heads of 128: 4 parts 144 us, 16 parts 145, 1 part MEASURED), for more rows once.
 FwdPlan fwd_plan(const AttnParams &P)
 {
     FwdPlan p;
-    p.few = P.max_rows <= 32;
-    p.tiles = p.few ? 1 : (P.max_rows + 127) / 128;
-    const int64_t groups = (int64_t)P.B * P.Hkv * p.tiles, key_tiles = p.few ? (P.max_k + 127) / 128 : (P.max_k + 63) / 64;
-    const int64_t want = 2 * (int64_t)cu_count();
+    const int64_t heads = (int64_t)P.B * P.Hkv, cus = cu_count(), full = heads * ((P.max_rows + 127) / 128);
+    const bool share = (full <= cus && P.max_k >= 512) || (P.D <= 64 && full <= 2 * cus && P.max_k >= 2048);
+    p.rows = P.max_rows <= 32 ? 32 : share ? 64 : 128;
+    p.tiles = (P.max_rows + p.rows - 1) / p.rows;
+    const int64_t groups = heads * p.tiles, key_tiles = (P.max_k + 63) / 64, want = (p.rows == 32 ? 2 : 1) * cus;
     p.splits = 1;
     if (groups < want) {
         p.splits = (want + groups - 1) / groups;
@@ -368,8 +431,8 @@ int sdrop_attn(const void *q, const void *k, const void *v, void *o, void *o_res
     P.part_o = static_cast<float *>(ws);
     P.part_lse = P.splits > 1 ? P.part_o + (int64_t)P.splits * P.B * P.Hkv * P.max_rows * P.D : nullptr;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (a->dtype == SDROP_F16) return P.D <= 64 ? launch_fwd<F16, 64>(P, p.few, st) : launch_fwd<F16, 128>(P, p.few, st);
-    return P.D <= 64 ? launch_fwd<BF16, 64>(P, p.few, st) : launch_fwd<BF16, 128>(P, p.few, st);
+    if (a->dtype == SDROP_F16) return P.D <= 64 ? launch_fwd<F16, 64>(P, p, st) : launch_fwd<F16, 128>(P, p, st);
+    return P.D <= 64 ? launch_fwd<BF16, 64>(P, p, st) : launch_fwd<BF16, 128>(P, p, st);
 }
 
 }  // extern "C"
