@@ -216,6 +216,17 @@ template <class T> __device__ __forceinline__ typename In<T>::vec narrow8(const 
     return __builtin_bit_cast(typename In<T>::vec, o);
 }
 
+// What that rounding took, rounded in turn.
+template <class T> __device__ __forceinline__ typename In<T>::vec narrow8_rest(const f32x16 &v, int part)
+{
+    typedef __attribute__((__vector_size__(8 * sizeof(typename In<T>::out16)))) typename In<T>::out16 e8;
+    e8 o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        o[i] = static_cast<typename In<T>::out16>(v[8 * part + i] - static_cast<float>(static_cast<typename In<T>::out16>(v[8 * part + i])));
+    return __builtin_bit_cast(typename In<T>::vec, o);
+}
+
 __device__ __forceinline__ f32x16 zero16()
 {
     f32x16 z;

@@ -32,6 +32,9 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? 2 : 1) void attn_fwd_k
     const int off = s.Lk - s.Lq;                    // causal: token i sees keys up to i + off
     const int r_last = min(R0 + 32 * QW, rows) - 1;
     const int k_end = P.causal ? min(s.Lk, token_of(P, r_last) + off + 1) : s.Lk;
+    // P is rounded for the second product.  Over many keys these errors average out; of rows that see few the backward pass would
+    // feel them (its row sums of dO O are to cancel sums of unrounded P dP): those get what the rounding took by a third product.
+    const bool whole_p = k_end <= 128;
     // this workgroup's part of the key tiles
     const int n_tiles = k_end > 0 ? (k_end + TKV - 1) / TKV : 0, per = (n_tiles + P.splits - 1) / P.splits;
     const int t0 = min(split * per, n_tiles), t1 = min(t0 + per, n_tiles);
@@ -110,6 +113,14 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? 2 : 1) void attn_fwd_k
             const typename In<T>::vec p = narrow8<T>(sc[ks >> 1], ks & 1);
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[d] = In<T>::mfma(va.get(0, d, ks), p, o[d]);
+        }
+        if (whole_p) {
+#pragma unroll
+            for (int ks = 0; ks < 2 * MB; ++ks) {
+                const typename In<T>::vec p = narrow8_rest<T>(sc[ks >> 1], ks & 1);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) o[d] = In<T>::mfma(va.get(0, d, ks), p, o[d]);
+            }
         }
     };
 
