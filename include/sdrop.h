@@ -596,8 +596,9 @@ int sdrop_layer_norm_bwd(const void *dY, const void *dH, const void *H, const vo
  *   k_len          NULL, or (without cu_k) device int32[B]: sequence b has k_len[b] <= max_k keys; what lies behind them is not read
  *   D              head size: a multiple of 8, at most 128
  *   lse            NULL, or fp32: [B, Hq, max_q], packed [Hq, total_q]
- *   o_rest         NULL, or an array like o (its strides, its alignment) that receives what o's rounding took, rounded in turn:
- *                  the backward pass needs row sums of dO O, whose error would otherwise be that of a rounded O
+ *   o_rest         NULL, or an array like o (its strides, its alignment) for the backward pass: the rows of tokens that see at most 128
+ *                  keys receive what o's rounding took, rounded in turn (the backward pass needs row sums of dO O, whose error would
+ *                  otherwise be that of a rounded O); the other rows are not written, and not read there
  *   ws, ws_bytes   sdrop_attn_workspace_bytes(a) bytes (partial results where few queries share many keys out to the whole
  *                  chip; may be 0), 16-byte aligned
  *

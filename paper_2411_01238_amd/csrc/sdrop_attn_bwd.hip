@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256, 2) void attn_dq_kernel(AttnParams P)
                 x = *reinterpret_cast<const uint4 *>(qp + 2 * col);
                 g = *reinterpret_cast<const uint4 *>(gp + 2 * col);
                 o = *reinterpret_cast<const uint4 *>(P.o + at + 2 * col);
-                if (P.rest) rest = *reinterpret_cast<const uint4 *>(P.rest + at + 2 * col);
+                if (P.rest && lim < kFewKeys) rest = *reinterpret_cast<const uint4 *>(P.rest + at + 2 * col);
             }
             qf[kk] = __builtin_bit_cast(typename In<T>::vec, x);
             gf[kk] = __builtin_bit_cast(typename In<T>::vec, g);

@@ -32,9 +32,7 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? 2 : 1) void attn_fwd_k
     const int off = s.Lk - s.Lq;                    // causal: token i sees keys up to i + off
     const int r_last = min(R0 + 32 * QW, rows) - 1;
     const int k_end = P.causal ? min(s.Lk, token_of(P, r_last) + off + 1) : s.Lk;
-    // P is rounded for the second product.  Over many keys these errors average out; of rows that see few the backward pass would
-    // feel them (its row sums of dO O are to cancel sums of unrounded P dP): those get what the rounding took by a third product.
-    const bool whole_p = k_end <= 128;
+    const bool whole_p = (P.causal ? token_of(P, R0) + off + 1 : s.Lk) <= kFewKeys;         // (of this tile's first row)
     // this workgroup's part of the key tiles
     const int n_tiles = k_end > 0 ? (k_end + TKV - 1) / TKV : 0, per = (n_tiles + P.splits - 1) / P.splits;
     const int t0 = min(split * per, n_tiles), t1 = min(t0 + per, n_tiles);
@@ -237,7 +235,7 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? 2 : 1) void attn_fwd_k
     const int64_t at = (P.cu_q ? 0 : b * P.o_b) + (s.q0 + i) * P.o_t + head * P.o_h;
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-        store_row32<T>(P.out + at + 64 * d, o[d], inv, P.D - 32 * d, live, P.out_rest ? P.out_rest + at + 64 * d : nullptr);
+        store_row32<T>(P.out + at + 64 * d, o[d], inv, P.D - 32 * d, live, P.out_rest && whole_p ? P.out_rest + at + 64 * d : nullptr, lim < kFewKeys);
     }
 }
 
@@ -294,7 +292,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams P)
             const e2 x = {static_cast<E>(a0 * inv), static_cast<E>(a1 * inv)};
             const int64_t at = (P.cu_q ? 0 : b * P.o_b) + (s.q0 + i) * P.o_t + head * P.o_h + 4 * lane;
             *reinterpret_cast<e2 *>(P.out + at) = x;
-            if (P.out_rest) {
+            if (P.out_rest && (P.causal ? min(s.Lk, i + s.Lk - s.Lq + 1) : s.Lk) <= kFewKeys) {
                 const e2 y = {static_cast<E>(a0 * inv - static_cast<float>(x[0])), static_cast<E>(a1 * inv - static_cast<float>(x[1]))};
                 *reinterpret_cast<e2 *>(P.out_rest + at) = y;
             }

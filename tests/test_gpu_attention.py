@@ -115,8 +115,11 @@ def test_few_queries_over_many_keys(B, Tq, Tk, Hq, Hkv, D, causal, dtype):
     o, lse = sdrop.sdrop_attn(q, k, v, causal, k_len=torch.tensor(lens, dtype=torch.int32, device="cuda"))
     for b, n in enumerate(lens):
         _check(q[b], k[b, :n], v[b, :n], None, causal, td, (o[b],), lse[b], "b=%d n=%d" % (b, n))
-    rest = sdrop.sdrop_attn(q, k, v, causal, k_len=torch.tensor(lens, dtype=torch.int32, device="cuda"), need_rest=True)
-    assert torch.equal(rest[0], o) and bool((rest[2].abs().float() <= torch.finfo(td).eps / 2 * o.abs().float() * 1.01 + 1e-6).all())
+    o2, _, rest = sdrop.sdrop_attn(q, k, v, causal, k_len=torch.tensor(lens, dtype=torch.int32, device="cuda"), need_rest=True)
+    assert torch.equal(o2, o)
+    for b, n in enumerate(lens):
+        if n + (Tq - 1 if not causal else 0) <= 128:        # what is kept of O's rounding: at most half a step
+            assert bool((rest[b].abs().float() <= torch.finfo(td).eps / 2 * o[b].abs().float() * 1.01 + 1e-6).all())
 
 
 @pytest.mark.parametrize("dtype", list(DT))
@@ -184,7 +187,7 @@ def test_strides_slices_and_other_orders():
     want = sdrop.sdrop_attn(q.contiguous(), k.contiguous(), v.contiguous(), True, 0.3, need_rest=True)
     out = torch.full((B, Hq, T, D), 7.0, dtype=td, device="cuda").transpose(1, 2)
     o, lse, rest = sdrop.sdrop_attn(q, k, v, True, 0.3, out=out, need_rest=True)
-    assert torch.equal(o, want[0]) and torch.equal(lse, want[1]) and torch.equal(rest, want[2])
+    assert torch.equal(o, want[0]) and torch.equal(lse, want[1]) and torch.equal(rest, want[2])     # (90 tokens: all of them are kept)
     g = sdrop.sdrop_attn_bwd(do.contiguous(), q.contiguous(), k.contiguous(), v.contiguous(), want[0], want[1], True, 0.3, rest=want[2])
     grad = torch.full((B, T, Hq + 2 * Hkv, D + 8), 7.0, dtype=td, device="cuda")
     outs = dict(out_dq=grad[:, :, :Hq, :D], out_dk=grad[:, :, Hq:Hq + Hkv, :D], out_dv=grad[:, :, Hq + Hkv:, :D])
@@ -269,7 +272,7 @@ def test_results_repeat_on_another_stream_and_in_a_graph():
 
     def step():
         o, lse, rest = sdrop.sdrop_attn(q, k, v, True, need_rest=True)
-        return (o, lse, rest) + sdrop.sdrop_attn_bwd(do, q, k, v, o, lse, True, rest=rest) + (sdrop.sdrop_attn(q[:, :1], cache_k, cache_v)[0],)
+        return (o, lse, rest[:, :128].clone()) + sdrop.sdrop_attn_bwd(do, q, k, v, o, lse, True, rest=rest) + (sdrop.sdrop_attn(q[:, :1], cache_k, cache_v)[0],)
 
     ref = [t.clone() for t in step()]
     side = torch.cuda.Stream()
