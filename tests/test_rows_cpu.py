@@ -70,3 +70,10 @@ def test_the_binding_refuses_what_is_no_gpu_matrix():
         sdrop.sdrop_dropout(x.double(), 0.5, 1)
     with pytest.raises(ValueError):
         sdrop.sdrop_dropout(x, 0.5, 1, residual=x.half())
+
+
+def test_models_refuse_unknown_operators():
+    from paper_2411_01238_amd import model_step as ms
+    for name in ("mlp", "gpt", "vit"):
+        with pytest.raises(ValueError):
+            ms.MODELS[name]("dense", 0.0, device="cpu", ops="other")
