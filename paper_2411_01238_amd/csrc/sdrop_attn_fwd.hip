@@ -324,7 +324,7 @@ template <class T, int HD> int launch_fwd(AttnParams P, const FwdPlan &p, hipStr
 // 8 heads of 128, no mask 41 -> 34, causal 34 -> 32; 4096 tokens, causal 76 -> 67; 2 x 2048, 16 heads of 64, causal 38 -> 32; but
 // 2 x 2048, 16 heads of 128, causal 55 -> 58; 32 x 128, 8 heads of 128, causal 12.1 -> 13.4.
 // Parts of the keys cost a pass over what they leave (12 us for 2048 rows of 8 heads): for few rows they fill the chip twice (16384
-// keys of 16 sequences, 8 heads of 128: 4 parts 144 us, 16 parts 145, 1 part MEASURED), for more rows once.
+// keys of 16 sequences, 8 heads of 128: 4 parts 144 us, 16 parts 145), for more rows once.
 FwdPlan fwd_plan(const AttnParams &P)
 {
     FwdPlan p;

@@ -128,9 +128,9 @@ template <class T, bool TAIL> __device__ __forceinline__ void chunk_y(const Norm
 
 // A row in the registers of WPR wavefronts, C chunks per lane: read once, the variance from the deviations.
 template <class T, int WPR, int C, bool TAIL>
-__global__ __launch_bounds__(256) void norm_fwd_kernel(NormArgs A)
+__global__ __launch_bounds__(WPR == 1 ? 256 : 64 * WPR) void norm_fwd_kernel(NormArgs A)
 {
-    __shared__ float red[2][4];
+    __shared__ float red[2][WPR];
     const int wave = threadIdx.x >> 6;
     const int t = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
     int64_t row = WPR == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
@@ -433,15 +433,18 @@ __global__ __launch_bounds__(256) void norm_finish_kernel(const float *part, W *
     }
 }
 
-// How a row lies in registers.  waves 0: it does not.
+// How a row lies in registers: the fewest wavefronts that leave a lane at most two chunks, since the backward pass holds five values for
+// each of its elements (32768 x 2048 bf16 on one wavefront, four chunks a lane: 102 us for dX alone, on four wavefronts 73; 8192 x 8192
+// on four wavefronts 91, on eight 74).  waves 0: it does not.
 struct RowPlan { int waves, chunks; };
 RowPlan row_plan(int64_t N)
 {
     if (N <= 512) return {1, 1};
     if (N <= 1024) return {1, 2};
-    if (N <= 2048) return {1, 4};
+    if (N <= 2048) return {4, 1};
     if (N <= 4096) return {4, 2};
-    if (N <= 8192) return {4, 4};
+    if (N <= 8192) return {8, 2};
+    if (N <= 16384) return {8, 4};
     return {0, 0};
 }
 
@@ -461,7 +464,8 @@ int64_t norm_parts(int64_t M, int64_t N)
     return most < 2 * cu_count() ? most : 2 * cu_count();
 }
 
-// (a launch counts its threads in 32 bits: kernels with a workgroup per row or per four rows walk on where there are more)
+// A launch counts its threads in 32 bits: kernels with a workgroup per row or per four rows walk on where there are more.  (Not
+// earlier: with 2048 workgroups, eight per CU, that walk over the rows 32768 x 2048 bf16 takes 128 us instead of 108.)
 constexpr int64_t kMostGroups = int64_t(1) << 22;
 unsigned groups_for(int64_t n) { return (unsigned)(n < kMostGroups ? n : kMostGroups); }
 
@@ -471,9 +475,10 @@ template <class T, bool TAIL> void launch_norm_fwd(const NormArgs &A, hipStream_
     const dim3 wave_rows(groups_for((A.M + 3) / 4)), rows(groups_for(A.M)), block(256);
     if (p.waves == 1 && p.chunks == 1) hipLaunchKernelGGL((norm_fwd_kernel<T, 1, 1, TAIL>), wave_rows, block, 0, st, A);
     else if (p.waves == 1 && p.chunks == 2) hipLaunchKernelGGL((norm_fwd_kernel<T, 1, 2, TAIL>), wave_rows, block, 0, st, A);
-    else if (p.waves == 1) hipLaunchKernelGGL((norm_fwd_kernel<T, 1, 4, TAIL>), wave_rows, block, 0, st, A);
-    else if (p.waves == 4 && p.chunks == 2) hipLaunchKernelGGL((norm_fwd_kernel<T, 4, 2, TAIL>), rows, block, 0, st, A);
-    else if (p.waves == 4) hipLaunchKernelGGL((norm_fwd_kernel<T, 4, 4, TAIL>), rows, block, 0, st, A);
+    else if (p.waves == 4 && p.chunks == 1) hipLaunchKernelGGL((norm_fwd_kernel<T, 4, 1, TAIL>), rows, block, 0, st, A);
+    else if (p.waves == 4) hipLaunchKernelGGL((norm_fwd_kernel<T, 4, 2, TAIL>), rows, block, 0, st, A);
+    else if (p.waves == 8 && p.chunks == 2) hipLaunchKernelGGL((norm_fwd_kernel<T, 8, 2, TAIL>), rows, dim3(512), 0, st, A);
+    else if (p.waves == 8) hipLaunchKernelGGL((norm_fwd_kernel<T, 8, 4, TAIL>), rows, dim3(512), 0, st, A);
     else hipLaunchKernelGGL((norm_fwd_long_kernel<T, TAIL>), rows, block, 0, st, A);
 }
 
@@ -483,9 +488,10 @@ template <class T, bool TAIL> void launch_norm_bwd(NormArgs A, int64_t parts, hi
     const dim3 grid((unsigned)parts), block(64 * kBwdWaves);
     if (p.waves == 1 && p.chunks == 1) hipLaunchKernelGGL((norm_bwd_kernel<T, 1, 1, TAIL>), grid, block, 0, st, A);
     else if (p.waves == 1 && p.chunks == 2) hipLaunchKernelGGL((norm_bwd_kernel<T, 1, 2, TAIL>), grid, block, 0, st, A);
-    else if (p.waves == 1) hipLaunchKernelGGL((norm_bwd_kernel<T, 1, 4, TAIL>), grid, block, 0, st, A);
-    else if (p.waves == 4 && p.chunks == 2) hipLaunchKernelGGL((norm_bwd_kernel<T, 4, 2, TAIL>), grid, block, 0, st, A);
-    else if (p.waves == 4) hipLaunchKernelGGL((norm_bwd_kernel<T, 4, 4, TAIL>), grid, block, 0, st, A);
+    else if (p.waves == 4 && p.chunks == 1) hipLaunchKernelGGL((norm_bwd_kernel<T, 4, 1, TAIL>), grid, block, 0, st, A);
+    else if (p.waves == 4) hipLaunchKernelGGL((norm_bwd_kernel<T, 4, 2, TAIL>), grid, block, 0, st, A);
+    else if (p.waves == 8 && p.chunks == 2) hipLaunchKernelGGL((norm_bwd_kernel<T, 8, 2, TAIL>), grid, block, 0, st, A);
+    else if (p.waves == 8) hipLaunchKernelGGL((norm_bwd_kernel<T, 8, 4, TAIL>), grid, block, 0, st, A);
     else {
         // the sums first: dr may be written over dy
         if (A.part) {
