@@ -66,12 +66,16 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? 2 : 1) void attn_fwd_k
     auto compute_keys = [&](int kv0, const char *kt, const char *vt) __attribute__((always_inline)) {
         f32x16 sc[MB];
         const RowOperand<HD, T> ka(kt);
+        // (a wavefront at its matrix instructions goes before the one beside it at its exponentials: 8192 tokens, 16 heads of 128, causal
+        // 305 -> 275 us)
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
             sc[mb] = zero16();
 #pragma unroll
             for (int kk = 0; kk < HD / 16; ++kk) sc[mb] = In<T>::mfma(ka.get(row_at<HD>(32) * mb, kk), qf[kk], sc[mb]);
         }
+        __builtin_amdgcn_s_setprio(0);
         if (kv0 + 32 * MB > s.Lk || (P.causal && kv0 + 32 * MB - 1 > w_first)) {
             const int last = lim - kv0 - 4 * h;
 #pragma unroll
@@ -106,12 +110,14 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? 2 : 1) void attn_fwd_k
                 l += sc[mb][e];
             }
         const ColOperand<HD, T> va(vt);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int ks = 0; ks < 2 * MB; ++ks) {
             const typename In<T>::vec p = narrow8<T>(sc[ks >> 1], ks & 1);
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[d] = In<T>::mfma(va.get(0, d, ks), p, o[d]);
         }
+        __builtin_amdgcn_s_setprio(0);
         if (whole_p) {
 #pragma unroll
             for (int ks = 0; ks < 2 * MB; ++ks) {
