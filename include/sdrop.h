@@ -595,6 +595,7 @@ int sdrop_layer_norm_bwd(const void *dY, const void *dH, const void *H, const vo
  *                  Rows behind the last sequence are left as they were.
  *   k_len          NULL, or (without cu_k) device int32[B]: sequence b has k_len[b] <= max_k keys; what lies behind them is not read
  *   D              head size: a multiple of 8, at most 128
+ *   scale          positive and finite, in fp32 as well
  *   lse            NULL, or fp32: [B, Hq, max_q], packed [Hq, total_q]
  *   o_rest         NULL, or an array like o (its strides, its alignment) for the backward pass: the rows of tokens that see at most 128
  *                  keys receive what o's rounding took, rounded in turn (the backward pass needs row sums of dO O, whose error would
@@ -602,6 +603,8 @@ int sdrop_layer_norm_bwd(const void *dY, const void *dH, const void *H, const vo
  *   ws, ws_bytes   sdrop_attn_workspace_bytes(a) bytes (partial results where few queries share many keys out to the whole
  *                  chip; may be 0), 16-byte aligned
  *
+ * o, o_rest and lse overlap no input.  Sizes: B <= 2^20, Hq <= 65536, B * Hq <= 2^24; max_q * Hq, max_k, total_q and total_k <= 2^30; B * Hkv
+ * times the tiles (of 32 to 128 rows or keys) of the longest sequence, times the parts of the keys, below 2^24.  Else SDROP_ESHAPE.
  * Offsets and lengths are device data: a sequence whose values do not fit the call (descending, beyond the array, longer than the
  * bound) is left out, nothing of it is read or written, and SDROP_STATUS_BAD_LENGTHS is set (see sdrop_status).
  */

@@ -26,6 +26,7 @@ def _desc(**kw):
 
 BAD = [
     (dict(scale=0.0), sdrop.EINVAL), (dict(scale=-1.0), sdrop.EINVAL), (dict(scale=float("inf")), sdrop.EINVAL), (dict(scale=float("nan")), sdrop.EINVAL),
+    (dict(scale=1e-60), sdrop.EINVAL), (dict(scale=1e300), sdrop.EINVAL), (dict(scale=3e38), sdrop.EINVAL),      # not in fp32 (the last: times log2 e)
     (dict(causal=2), sdrop.EINVAL), (dict(dtype=sdrop.F32), sdrop.EDTYPE), (dict(dtype=9), sdrop.EDTYPE),
     (dict(B=0), sdrop.ESHAPE), (dict(max_q=0), sdrop.ESHAPE), (dict(max_k=0), sdrop.ESHAPE), (dict(Hq=3), sdrop.ESHAPE), (dict(Hkv=0), sdrop.ESHAPE),
     (dict(D=0), sdrop.ESHAPE), (dict(D=60), sdrop.ESHAPE), (dict(D=136), sdrop.ESHAPE), (dict(max_q=1 << 31), sdrop.ESHAPE), (dict(max_q=1 << 29), sdrop.ESHAPE),
