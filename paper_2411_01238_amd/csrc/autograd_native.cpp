@@ -16,13 +16,14 @@ using torch::autograd::AutogradContext;
 using torch::autograd::variable_list;
 using OptTensor = std::optional<Tensor>;
 
-struct Failure {
+struct Failure : std::runtime_error {
     int code;
-    const char *what;
+    const char *call;
+    Failure(int rc, const char *name) : std::runtime_error(name), code(rc), call(name) {}
 };
 void check(int rc, const char *what)
 {
-    if (rc != SDROP_OK) throw Failure{rc, what};
+    if (rc != SDROP_OK) throw Failure(rc, what);
 }
 void require(bool ok, const char *what)
 {
@@ -42,7 +43,7 @@ int type_code(const Tensor &t, const char *what)
     case torch::kHalf: return SDROP_F16;
     case torch::kBFloat16: return SDROP_BF16;
     case torch::kFloat: return SDROP_F32;
-    default: throw Failure{SDROP_EDTYPE, what};
+    default: throw Failure(SDROP_EDTYPE, what);
     }
 }
 
@@ -65,13 +66,23 @@ struct Rows {
     void *ptr() const { return t.data_ptr(); }
 };
 
-// A gradient cannot be differentiated once more: where a graph of it is asked for, the error waits at its end.
-variable_list once(variable_list &&out)
+// A gradient cannot be differentiated once more: where a graph of it is asked for, the error waits between it and the tensors `of`
+// that it was computed from.
+variable_list once(variable_list &&out, const variable_list &of)
 {
     if (!at::GradMode::is_enabled()) return std::move(out);
+    const size_t n = out.size();
+    out.insert(out.end(), of.begin(), of.end());
     auto node = std::make_shared<torch::autograd::DelayedError>("libsdrop's operators can be differentiated once", (int)out.size());
     node->set_next_edges(torch::autograd::edge_list());
-    return (*node)(std::move(out));
+    variable_list res = (*node)(std::move(out));
+    res.resize(n);
+    return res;
+}
+variable_list joined(variable_list a, const variable_list &b)
+{
+    a.insert(a.end(), b.begin(), b.end());
+    return a;
 }
 
 uint64_t bits(const c10::IValue &v) { return (uint64_t)v.toInt(); }
@@ -114,7 +125,7 @@ struct Dropout : torch::autograd::Function<Dropout> {
             dx = drop(Rows(g[0]), nullptr, ctx->saved_data["p"].toDouble(), bits(ctx->saved_data["seed"]), bits(ctx->saved_data["stream"]), rc);
             check_backward(rc, "sdrop_dropout");
         }
-        return once({dx, ctx->saved_data["residual"].toBool() ? g[0] : Tensor(), Tensor(), Tensor(), Tensor()});
+        return once({dx, ctx->saved_data["residual"].toBool() ? g[0] : Tensor(), Tensor(), Tensor(), Tensor()}, g);
     }
 };
 
@@ -191,7 +202,7 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
             at::AutoDispatchBelowADInplaceOrView guard;
             norm_backward(g[0], Tensor(), s[0], s[1], s[2], 0.0, 0, 0, nx, false, nw, nb, out);
         }
-        return once({out[0], out[2], out[3], Tensor()});
+        return once({out[0], out[2], out[3], Tensor()}, joined(g, s));
     }
 };
 
@@ -238,7 +249,7 @@ struct DropoutAddNorm : torch::autograd::Function<DropoutAddNorm> {
                 if (nr) out[1] = g[1];
             }
         }
-        return once({out[0], out[1], out[2], out[3], Tensor(), Tensor(), Tensor(), Tensor()});
+        return once({out[0], out[1], out[2], out[3], Tensor(), Tensor(), Tensor(), Tensor()}, joined(g, s));
     }
 };
 
@@ -385,7 +396,7 @@ struct Attention : torch::autograd::Function<Attention> {
             dv = like(s[2], a.cu_k.has_value());
             attn_backward(g[0], s[0], s[1], s[2], s[3], s[4], s[5], a, dq, dk, dv);
         }
-        return once({dq, dk, dv, Tensor()});
+        return once({dq, dk, dv, Tensor()}, joined(g, s));
     }
 };
 
@@ -421,7 +432,7 @@ struct QkvAttention : torch::autograd::Function<QkvAttention> {
             auto part = [&](const Tensor &t, int i) { return i == 0 ? t.narrow(-2, 0, hq) : t.narrow(-2, hq + (i - 1) * hkv, hkv); };
             attn_backward(g[0], part(s[0], 0), part(s[0], 1), part(s[0], 2), s[1], s[2], s[3], a, part(d, 0), part(d, 1), part(d, 2));
         }
-        return once({d, Tensor(), Tensor()});
+        return once({d, Tensor(), Tensor()}, joined(g, s));
     }
 };
 
@@ -442,7 +453,7 @@ PYBIND11_MODULE(_native, m)
             if (e) std::rethrow_exception(e);
         } catch (const Failure &f) {
             pybind11::object cls = pybind11::module_::import("paper_2411_01238_amd.sdrop").attr("SdropError");
-            PyErr_SetObject(cls.ptr(), cls(f.code, f.what).ptr());
+            PyErr_SetObject(cls.ptr(), cls(f.code, f.call).ptr());
         }
     });
     m.def("dropout", [](const Tensor &x, const OptTensor &residual, double p, uint64_t seed, uint64_t stream) {

@@ -329,3 +329,74 @@ def test_block_of_operators_trains():
     tol = 12 * torch.finfo(td).eps
     for a, b in [(y, yr)] + list(zip(got, want)):
         assert (a.detach().cpu().double() - b.detach()).norm() <= tol * b.detach().norm()
+
+
+def test_block_captured_with_its_backward_pass():
+    # all operators and their gradients through autograd, captured; no eager graph of the leaves lives meanwhile
+    td = torch.bfloat16
+    B, T, H, D = 2, 150, 4, 64
+    x, r = _randn((B, T, 3 * H * D), td, 1).requires_grad_(), _randn((B, T, H * D), td, 2).requires_grad_()
+    w3, w1 = _randn((3 * H * D,), td, 3).requires_grad_(), _randn((H * D,), td, 4).requires_grad_()
+    gy, gz = _randn((B, T, H * D), td, 5), _randn((B, T, H * D), td, 6)
+    leaves = (x, r, w3, w1)
+
+    def step():
+        a = tr.qkv_attention(tr.layer_norm(x, w3).view(B, T, 3 * H, D), H, causal=True).view(B, T, H * D)
+        y, h = tr.dropout_add_norm(a, r, w1, None, 0.2, 1e-5, 7, 8)
+        z = tr.dropout(y, 0.3, 7, 9, residual=h)
+        return [y.detach(), z.detach()] + list(torch.autograd.grad((y, z), leaves, (gy, gz)))
+
+    ref = [t.clone() for t in step()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    for a, c in zip(ref, other):
+        assert torch.equal(a, c)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        outs = step()
+    for _ in range(3):
+        for o in outs:
+            o.fill_(7.0)
+        step()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for o, c in zip(outs, ref):
+            assert torch.equal(o, c)
+
+
+def test_gradients_refuse_to_be_differentiated_again():
+    x = _randn((2, 20, 6, 64), torch.bfloat16, 1).requires_grad_()
+    w = _randn((64,), torch.bfloat16, 2).requires_grad_()
+    forms = [lambda: tr.dropout(x, 0.5, 1), lambda: tr.layer_norm(x, w), lambda: tr.dropout_add_norm(x, x, w, None, 0.5)[0],
+             lambda: tr.attention(x, x, x), lambda: tr.qkv_attention(x, 2)]
+    for f in forms:
+        y = f()
+        g, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+        plain, = torch.autograd.grad((f().detach() * 2 * f()).sum(), x)
+        assert g.requires_grad and torch.equal(g, plain)
+        with pytest.raises(RuntimeError, match="differentiated once"):
+            torch.autograd.grad(g.sum(), x)
+        with pytest.raises(RuntimeError, match="differentiated once"):
+            g.sum().backward()
+
+
+def test_two_streams_at_once():
+    # two calls that overlap, each with partial results of its own
+    td = torch.float16
+    q, k, v = _randn((1, 1, 8, 128), td, 1), _randn((1, 30000, 8, 128), td, 2), _randn((1, 30000, 8, 128), td, 3)
+    want = [sdrop.sdrop_attn(q, k, v)[0], sdrop.sdrop_attn(q, v, k)[0]]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(8):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(sdrop.sdrop_attn(q, *((k, v) if i == 0 else (v, k)))[0])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(t, want[i]) for t in got[i])
