@@ -763,10 +763,12 @@ def sdrop_col_sum(dY, out=None, ws=None):
 
 # ---- around the substituted layers: element dropout, layer norm ----
 
-def _on_current_device(t):
+def _on_current_device(*tensors):
     """Launches go to the current device's stream: a tensor of another device is refused here (its kernels would fault there)."""
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError("tensors must be on the current device: call under torch.cuda.device(%d)" % t.device.index)
+    at = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise ValueError("tensors must be on the current device, %d: call under torch.cuda.device(%d)" % (at, t.get_device()))
 
 
 def _row_types(name, x, *others):
@@ -805,7 +807,7 @@ def sdrop_dropout(X, p, seed, rng_stream=0, residual=None, out=None):
     if out is None:
         out = torch.empty((M, N), dtype=X.dtype, device=X.device)
     (px, ldx), (pr, ldr), (po, ldo) = _mat(X, "X"), _opt_mat(residual, "residual", (M, N)), _opt_mat(out, "out", (M, N))
-    _on_current_device(X)
+    _on_current_device(X, residual, out)
     _check(lib().sdrop_dropout(px, pr, po, M, N, float(p), int(seed), int(rng_stream), dt, ldx, ldr, ldo, _stream()), "sdrop_dropout")
     return out
 
@@ -827,7 +829,7 @@ def sdrop_layer_norm(X, gamma, beta=None, eps=1e-5, residual=None, p=0.0, seed=0
     (px, ldx), (pr, ldr) = _mat(X, "X"), _opt_mat(residual, "residual", (M, N))
     (ph, ldh), (py, ldy) = _opt_mat(out_h, "out_h", (M, N)), _opt_mat(out, "out", (M, N))
     pg, pb = _weight(gamma, "gamma", N, X.dtype), _weight(beta, "beta", N, X.dtype)
-    _on_current_device(X)
+    _on_current_device(X, residual, gamma, beta, out, out_h)
     at = stats.data_ptr()
     _check(lib().sdrop_layer_norm(px, pr, pg, pb, ph, py, at, at + 4 * M, M, N, float(eps), float(p), int(seed), int(rng_stream),
                                   dt, _DTYPES[gamma.dtype], ldx, ldr, ldh, ldy, _stream()), "sdrop_layer_norm")
@@ -854,7 +856,7 @@ def sdrop_layer_norm_bwd(dY, H, gamma, mean, rstd, dH=None, p=0.0, seed=0, rng_s
         ws = torch.empty(max(int(lib().sdrop_layer_norm_bwd_workspace_bytes(M, N)), 16), dtype=torch.uint8, device=dY.device)
     (py, ldy), (pdh, lddh), (ph, ldh) = _mat(dY, "dY"), _opt_mat(dH, "dH", (M, N)), _opt_mat(H, "H", (M, N))
     pg, at = _weight(gamma, "gamma", N, dY.dtype), [None if t is None else t.data_ptr() for t in (dr, dx, dg, db)]
-    _on_current_device(dY)
+    _on_current_device(dY, dH, H, gamma, mean, rstd, ws)
     _check(lib().sdrop_layer_norm_bwd(py, pdh, ph, pg, _dev(mean, "mean"), _dev(rstd, "rstd"), *at, M, N, float(p), int(seed), int(rng_stream),
                                       dt, _DTYPES[gamma.dtype], ldy, lddh, ldh, 0, 0, None if ws is None else ws.data_ptr(),
                                       0 if ws is None else ws.numel() * ws.element_size(), _stream()), "sdrop_layer_norm_bwd")
@@ -905,6 +907,7 @@ def _attn_desc(q, k, v, causal, scale, cu_q, cu_k, max_q, max_k, k_len):
     pq, (a.q_b, a.q_t, a.q_h) = _heads(q, "q", q.shape[:-2], Hq, D, q.dtype)
     pk, (a.k_b, a.k_t, a.k_h) = _heads(k, "k", lead_k, Hkv, D, q.dtype)
     pv, (a.v_b, a.v_t, a.v_h) = _heads(v, "v", lead_k, Hkv, D, q.dtype)
+    _on_current_device(q, k, v, cu_q, cu_k, k_len)
     return a, pq, pk, pv
 
 
@@ -926,7 +929,7 @@ def sdrop_attn(q, k, v, causal=False, scale=None, cu_q=None, cu_k=None, max_q=No
     lse = None
     if need_lse:
         lse = torch.empty((a.B, a.Hq, a.max_q) if cu_q is None else (a.Hq, a.total_q), dtype=torch.float32, device=q.device)
-    _on_current_device(q)
+    _on_current_device(out, ws)
     L = lib()
     ref = ctypes.byref(a)
     need = L.sdrop_attn_workspace_bytes(ref)
@@ -957,7 +960,7 @@ def sdrop_attn_bwd(dO, q, k, v, O, lse, causal=False, scale=None, cu_q=None, cu_
     pdq, (a.dq_b, a.dq_t, a.dq_h) = _heads(out_dq, "out_dq", lead_q, a.Hq, a.D, q.dtype)
     pdk, (a.dk_b, a.dk_t, a.dk_h) = _heads(out_dk, "out_dk", lead_k, a.Hkv, a.D, q.dtype)
     pdv, (a.dv_b, a.dv_t, a.dv_h) = _heads(out_dv, "out_dv", lead_k, a.Hkv, a.D, q.dtype)
-    _on_current_device(q)
+    _on_current_device(dO, O, lse, rest, out_dq, out_dk, out_dv, ws)
     L = lib()
     ref = ctypes.byref(a)
     if ws is None:

@@ -3,11 +3,17 @@ modules: element dropout, layer norm, dropout + residual add + layer norm in one
 kernels; the autograd nodes around them are in csrc/autograd_native.cpp.  Each can be differentiated once.
 
 The dropout's mask is a function of a seed and a stream number (`rng_stream`: one per call, e.g. a step counter) and is never
-stored: the backward pass draws it again.  A captured graph replays the mask of the numbers it was captured with.
+stored: the backward pass draws it again.  A captured graph replays the mask of the numbers it was captured with; a module that is run
+again to save memory draws a new mask: use the functions there, with a stream number of the step's own.  Capture a backward pass only
+after the eager graphs of the same leaves are gone (torch would add their gradients on those graphs' stream, outside the capture).
 """
 import torch
 
-from . import _native
+try:
+    from . import _native
+except ImportError as e:
+    raise RuntimeError("_native.so is not built or does not fit this torch: run `python -m paper_2411_01238_amd.build` "
+                       "(there is no fallback path)") from e
 
 _U64 = (1 << 64) - 1
 
