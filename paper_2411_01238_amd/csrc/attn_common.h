@@ -78,6 +78,14 @@ __device__ __forceinline__ int token_of(const AttnParams &P, int r)
     return (int)((__umulhi((uint32_t)r, P.g_mul) + (uint32_t)r) >> P.g_shift);
 }
 
+// The lane's number from nothing: what is worked out of threadIdx.x the compiler would keep in registers over a loop instead.
+__device__ __forceinline__ int lane_again()
+{
+    int ones = -1;
+    asm volatile("" : "+s"(ones));
+    return __builtin_amdgcn_mbcnt_hi(ones, __builtin_amdgcn_mbcnt_lo(ones, 0));
+}
+
 // Workgroup id -> (sequence and key head, unit).  Consecutive workgroups go to the eight XCDs in turn.
 // Where all units cost the same: eight heads at a time, one for each XCD, so that the workgroups that read the same keys share
 // an L2.  Where they do not (a causal mask, sequences of different lengths): the first unit of every head, then the second, the
@@ -100,14 +108,15 @@ __device__ __forceinline__ void place(const AttnParams &P, int units, int &bh, i
 // ---- tiles in LDS: [rows][HD] of 16-bit values ----
 //
 // One load instruction of a wavefront fills 1 KiB, 4 rows of 128 values or 8 of 64; such groups lie 1040 bytes apart.  In a group 16-byte
-// chunk c of row r lies in slot c ^ swz_a(r).  Operands are read along the rows (ds_read_b128: 16 consecutive rows, one chunk) and
-// across them (ds_read_b64_tr_b16: 4 consecutive rows x 64 bytes): the XOR keeps the rows of a group apart and the 16 bytes between groups
-// the groups, so that either read is spread over all banks (no conflicts, counted).  An XOR of all 16 rows' bits would do the same
-// without the gap, but leave twice as many lane addresses to be made or kept.
+// chunk c of row r lies in slot c ^ swz_a(r).  Operands are read along the rows (ds_read_b128: one chunk, 16 rows at a time: 0 .. 3, 12 .. 15
+// and 20 .. 27, then those between) and across them (ds_read_b64_tr_b16: 4 consecutive rows x 64 bytes): the XOR keeps four rows apart and
+// the 16 bytes between groups the fours, so that either read is spread over all banks (no conflicts, counted; rows of 64 values told apart
+// by their third bit too collided with the fours behind, a third of LDS's cycles: 2 x 4096, 16 heads, no mask, forward 173 -> 166 us).
+// An XOR of all 16 rows' bits would do the same without the gap, but leave twice as many lane addresses to be made or kept.
 template <int HD> constexpr int tile_bytes(int rows) { return rows * HD / 512 * 1040; }
 template <int HD> __device__ __forceinline__ constexpr int swz_a(int r)
 {
-    return HD >= 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2 | ((r >> 2) & 1) << 1;
+    return HD >= 128 ? (r & 3) << 2 : ((r >> 1) & 1) << 2;
 }
 // byte offset of row r (without its chunk)
 template <int HD> __device__ __forceinline__ constexpr int row_at(int r)
@@ -138,11 +147,14 @@ template <int HD, int ROWS, int NW> struct TileLoad {
 #pragma unroll
             for (int i = 0; i < PASSES; ++i, base += RPI * NW * stride) dma16(base, voff, lds + (wave + NW * i) * 1040);
         } else {
+            // (made here: four registers that would be kept for the whole loop)
+            uint4 zero = make_uint4(0, 0, 0, 0);
+            asm volatile("" : "+v"(zero.x), "+v"(zero.y), "+v"(zero.z), "+v"(zero.w));
 #pragma unroll
             for (int i = 0; i < PASSES; ++i, base += RPI * NW * stride) {
                 char *const dst = lds + (wave + NW * i) * 1040;
                 if (row + RPI * NW * i < rows && chunk < nch) dma16(base, voff, dst);
-                else *reinterpret_cast<uint4 *>(dst + (threadIdx.x & 63) * 16) = make_uint4(0, 0, 0, 0);
+                else *reinterpret_cast<uint4 *>(dst + lane_again() * 16) = zero;
             }
         }
     }
@@ -184,7 +196,7 @@ template <int HD, class T> struct RowOperand {
     __device__ __forceinline__ typename In<T>::vec get(int offset, int kk) const
     {
         // (of the bits that the XOR leaves alone the address is a sum)
-        constexpr int PLAIN = HD >= 128 ? 32 : 0;
+        constexpr int PLAIN = 32;
         return *reinterpret_cast<const typename In<T>::vec *>(at + (f ^ ((kk << 5) & ~PLAIN)) + ((kk << 5) & PLAIN) + offset);
     }
 };
@@ -256,7 +268,7 @@ template <class T> __device__ __forceinline__ void store_row32(char *p, const f3
 {
     using E = typename In<T>::out16;
     typedef __attribute__((__vector_size__(4 * sizeof(E)))) E e4;
-    const int h = (threadIdx.x >> 5) & 1;
+    const int h = lane_again() >> 5;
     auto put = [&](char *to, e4 a, e4 b, int g, bool live) __attribute__((always_inline)) {
         const uint2 x = __builtin_bit_cast(uint2, a), y = __builtin_bit_cast(uint2, b);
         const auto s = __builtin_amdgcn_permlane32_swap(x.x, y.x, false, false), t = __builtin_amdgcn_permlane32_swap(x.y, y.y, false, false);

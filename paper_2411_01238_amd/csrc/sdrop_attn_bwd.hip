@@ -38,9 +38,10 @@ template <class T> __device__ __forceinline__ float dot8(uint4 a, uint4 b, float
 // dQ.  As in the forward pass a lane holds keys of one query: S^T = K Q^T, dP^T = V dO^T, dQ^T = K^T dS^T; lse and delta are one number
 // per lane each.
 // QW wavefronts own rows of their own; the 4 / QW wavefronts of the same rows take a tile's blocks of 32 keys in turn and are joined at
-// the end.
+// the end.  Heads of 64 leave room for four wavefronts per SIMD, whose products run beside each other's exponentials (24 sequences of 64
+// to 2000 tokens, 16 heads, 4 of keys, causal, the whole backward pass: 394 -> 377 us).
 template <class T, int HD, int QW>
-__global__ __launch_bounds__(256, HD <= 64 && QW == 2 ? 4 : 2) void attn_dq_kernel(AttnParams P)
+__global__ __launch_bounds__(256, HD <= 64 ? 4 : 2) void attn_dq_kernel(AttnParams P)
 {
     constexpr int TKV = 64, TILE = tile_bytes<HD>(TKV), DB = HD / 32, KW = 4 / QW, ROWS = 32 * QW;
     __shared__ __attribute__((aligned(1024))) char lds[4 * TILE];
@@ -385,11 +386,13 @@ bool few_key_tiles(const AttnParams &P)
 }
 
 // dQ on 64 rows a workgroup, two wavefronts sharing out the keys of the same rows, instead of 128.  us, 128 -> 64: 2048 tokens, 8
-// heads of 128, no mask 65 -> 44, causal 62 -> 40; 4096 tokens, causal 121 -> 86; heads of 64: 2 x 2048, 16 heads, causal 53 -> 44, 4 x 2048
-// 95 -> 77, 2 x 4096, no mask 271 -> 252; but 2 x 4096, 16 heads of 128 257 -> 282, 32 x 128, 8 heads of 128 18.5 -> 20.0.
+// heads of 128, no mask 65 -> 44, causal 62 -> 40; 4096 tokens, causal 121 -> 86; but 2 x 4096, 16 heads of 128 257 -> 282, 32 x 128, 8
+// heads of 128 18.5 -> 20.0.  16 heads of 64 (the whole backward pass): 2 x 2048, causal 100 -> 93, 8192 tokens, causal 531 -> 522; but
+// 2 x 4096, no mask 521 -> 530, 4 x 4096, 4 key heads, causal 587 -> 600.
 bool few_rows(const AttnParams &P)
 {
-    return (P.max_k >= 512 && (int64_t)P.B * P.Hkv * ((P.max_rows + 127) / 128) <= cu_count()) || (P.D <= 64 && P.max_k >= 2048);
+    const int64_t full = (int64_t)P.B * P.Hkv * ((P.max_rows + 127) / 128), cus = cu_count();
+    return (P.max_k >= 512 && full <= cus) || (P.D <= 64 && P.causal && P.max_k >= 2048 && full <= 4 * cus);
 }
 
 template <class T, int HD> int launch_bwd(AttnParams P, hipStream_t st)

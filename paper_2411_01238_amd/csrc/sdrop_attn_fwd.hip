@@ -14,8 +14,11 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // QW: wavefronts of the workgroup that own rows of their own (32 each); KW (1 or 2) wavefronts of the same rows take the keys of a tile in
 // turn and are joined at the end.  MB: blocks of 32 keys per wavefront and tile.  STAGES: tiles that LDS holds.
+// Heads of 64 are bound by the exponentials: four wavefronts per SIMD, so that products run beside them (2 x 4096, 16 heads, no mask 171 ->
+// 158 us; 24 sequences of 64 to 2000 tokens, 16 heads, 4 of keys, causal 121 -> 104).  That leaves 128 registers, hence operands that
+// are read two ahead of the matrix instructions and no more.
 template <class T, int HD, int QW, int KW, int MB, int STAGES>
-__global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? 2 : 1) void attn_fwd_kernel(AttnParams P)
+__global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? (HD <= 64 ? 4 : 2) : 1) void attn_fwd_kernel(AttnParams P)
 {
     constexpr int TKV = 32 * MB * KW, TILE = tile_bytes<HD>(TKV), DB = HD / 32;
     __shared__ __attribute__((aligned(1024))) char lds[STAGES * 2 * TILE];
@@ -75,6 +78,16 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? 2 : 1) void attn_fwd_k
 #pragma unroll
             for (int kk = 0; kk < HD / 16; ++kk) sc[mb] = In<T>::mfma(ka.get(row_at<HD>(32) * mb, kk), qf[kk], sc[mb]);
         }
+        if constexpr (HD <= 64 && MB == 2) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+            for (int i = 0; i < MB * HD / 16 - 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         __builtin_amdgcn_s_setprio(0);
         if (kv0 + 32 * MB > s.Lk || (P.causal && kv0 + 32 * MB - 1 > w_first)) {
             const int last = lim - kv0 - 4 * h;
@@ -110,12 +123,23 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? 2 : 1) void attn_fwd_k
                 l += sc[mb][e];
             }
         const ColOperand<HD, T> va(vt);
+        if constexpr (HD <= 64 && MB == 2) __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int ks = 0; ks < 2 * MB; ++ks) {
             const typename In<T>::vec p = narrow8<T>(sc[ks >> 1], ks & 1);
 #pragma unroll
             for (int d = 0; d < DB; ++d) o[d] = In<T>::mfma(va.get(0, d, ks), p, o[d]);
+        }
+        if constexpr (HD <= 64 && MB == 2) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+            for (int i = 0; i < 2 * MB * DB - 2; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_s_setprio(0);
         if (whole_p) {
@@ -220,28 +244,32 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? 2 : 1) void attn_fwd_k
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[d][e] = o[d][e] * f0 + ob[(d * 16 + e) * 64] * f1;
     }
+    // (this lane's row once more: kept over the loop it would be registers that the fourth wavefront of a SIMD does not leave)
+    const int ln = lane_again(), r_out = R0 + 32 * wq + (ln & 31), h_out = ln >> 5;
+    const int r_in = min(r_out, rows - 1), i_out = token_of(P, r_in), head_out = hkv * P.G + (r_in - i_out * P.G);
+    const bool live_out = r_out < rows;
     const float inv = l > 0.f ? 1.f / l : l == l ? 0.f : l;         // (no key seen: 0; NaN stays NaN)
     const float lse = l > 0.f || l != l ? (m * P.c + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
     if (P.splits > 1) {
-        const int64_t row = ((int64_t)split * P.B * P.Hkv + bh) * P.max_rows + r;
-        if (live && h == 0) P.part_lse[row] = lse;
+        const int64_t row = ((int64_t)split * P.B * P.Hkv + bh) * P.max_rows + r_out;
+        if (live_out && h_out == 0) P.part_lse[row] = lse;
         float *const dst = P.part_o + row * P.D;
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int col = 32 * d + 8 * g + 4 * h;
+                const int col = 32 * d + 8 * g + 4 * h_out;
                 const f32q x = {o[d][4 * g] * inv, o[d][4 * g + 1] * inv, o[d][4 * g + 2] * inv, o[d][4 * g + 3] * inv};
-                if (live && col < P.D) *reinterpret_cast<f32q *>(dst + col) = x;
+                if (live_out && col < P.D) *reinterpret_cast<f32q *>(dst + col) = x;
             }
         }
         return;
     }
-    if (P.lse && live && h == 0) P.lse[P.cu_q ? head * P.total_q + s.q0 + i : ((int64_t)b * P.Hq + head) * P.max_q + i] = lse;
-    const int64_t at = (P.cu_q ? 0 : b * P.o_b) + (s.q0 + i) * P.o_t + head * P.o_h;
+    if (P.lse && live_out && h_out == 0) P.lse[P.cu_q ? head_out * P.total_q + s.q0 + i_out : ((int64_t)b * P.Hq + head_out) * P.max_q + i_out] = lse;
+    const int64_t at = (P.cu_q ? 0 : b * P.o_b) + (s.q0 + i_out) * P.o_t + head_out * P.o_h;
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-        store_row32<T>(P.out + at + 64 * d, o[d], inv, P.D - 32 * d, live, P.out_rest && whole_p ? P.out_rest + at + 64 * d : nullptr, lim < kFewKeys);
+        store_row32<T>(P.out + at + 64 * d, o[d], inv, P.D - 32 * d, live_out, P.out_rest && whole_p ? P.out_rest + at + 64 * d : nullptr, (P.causal ? i_out + off : s.Lk - 1) < kFewKeys);
     }
 }
 
