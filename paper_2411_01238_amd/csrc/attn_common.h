@@ -26,6 +26,7 @@ struct AttnParams {
     int32_t tiles, splits;                  // row tiles of the longest sequence; parts of the keys
     uint32_t g_mul;                         // r / G = (mulhi(r, g_mul) + r) >> g_shift
     int32_t g_shift;
+    int32_t steady;                         // backward: 16 rows are whole tokens (G divides 16), 32 rows lie within 31 bits of bytes
     float scale, c;                         // c = scale * log2(e)
     int *status;
 };

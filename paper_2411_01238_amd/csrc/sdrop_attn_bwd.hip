@@ -231,17 +231,31 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnParams P)
         asm volatile("" : "+v"(ln));
         const int lrow = RPI * wave + (ln * 16) / ROW_BYTES, chunk = ((ln * 16) % ROW_BYTES >> 4) ^ swz_a<HD>(lrow);
         char *const dst = lds + buf * 2 * TILE;
+        if (P.steady && (t + 1) * TQ <= rows && nch == HD / 8) {
+            // every pass has the same heads of the group, tokens further on: 32-bit offsets from addresses that the lanes share
+            const int tok = lrow >> P.g_shift, g = lrow & (P.G - 1), t_tok = t * TQ >> P.g_shift, step = RPI * 4 >> P.g_shift;
+            const uint32_t qo = (uint32_t)tok * (uint32_t)P.q_t + (uint32_t)g * (uint32_t)P.q_h + chunk * 16;
+            const uint32_t go = (uint32_t)tok * (uint32_t)P.do_t + (uint32_t)g * (uint32_t)P.do_h + chunk * 16;
+            const char *q_at = qb + t_tok * P.q_t, *g_at = gb + t_tok * P.do_t;
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const int rr = t * TQ + lrow + RPI * 4 * p;
-            char *const at = dst + (wave + 4 * p) * 1040;
-            if (rr < rows && chunk < nch) {
-                const int tok = token_of(P, rr), g = rr - tok * P.G;
-                dma16_at(qb + tok * P.q_t + g * P.q_h + chunk * 16, at);
-                dma16_at(gb + tok * P.do_t + g * P.do_h + chunk * 16, at + TILE);
-            } else {
-                *reinterpret_cast<uint4 *>(at + ln * 16) = make_uint4(0, 0, 0, 0);
-                *reinterpret_cast<uint4 *>(at + TILE + ln * 16) = make_uint4(0, 0, 0, 0);
+            for (int p = 0; p < PASSES; ++p, q_at += step * P.q_t, g_at += step * P.do_t) {
+                char *const at = dst + (wave + 4 * p) * 1040;
+                dma16(q_at, qo, at);
+                dma16(g_at, go, at + TILE);
+            }
+        } else {
+#pragma unroll
+            for (int p = 0; p < PASSES; ++p) {
+                const int rr = t * TQ + lrow + RPI * 4 * p;
+                char *const at = dst + (wave + 4 * p) * 1040;
+                if (rr < rows && chunk < nch) {
+                    const int tok = token_of(P, rr), g = rr - tok * P.G;
+                    dma16_at(qb + tok * P.q_t + g * P.q_h + chunk * 16, at);
+                    dma16_at(gb + tok * P.do_t + g * P.do_h + chunk * 16, at + TILE);
+                } else {
+                    *reinterpret_cast<uint4 *>(at + ln * 16) = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4 *>(at + TILE + ln * 16) = make_uint4(0, 0, 0, 0);
+                }
             }
         }
         if (threadIdx.x < TQ / 2) dma16_at(stats + (int64_t)t * TQ * 8 + ln * 16, lds + 4 * TILE + buf * TQ * 8);
@@ -455,6 +469,8 @@ int sdrop_attn_bwd(const void *dO, const void *q, const void *k, const void *v, 
     P.dk = static_cast<char *>(dk);
     P.dv = static_cast<char *>(dv);
     P.delta = static_cast<float *>(ws);
+    auto narrow = [&](int64_t t, int64_t h) { return (P.G - 1) * h + 32 / P.G * t < (int64_t(1) << 31); };
+    P.steady = 16 % P.G == 0 && narrow(P.q_t, P.q_h) && narrow(P.do_t, P.do_h);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (a->dtype == SDROP_F16) return P.D <= 64 ? launch_bwd<F16, 64>(P, st) : launch_bwd<F16, 128>(P, st);
     return P.D <= 64 ? launch_bwd<BF16, 64>(P, st) : launch_bwd<BF16, 128>(P, st);
