@@ -595,7 +595,7 @@ int sdrop_layer_norm_bwd(const void *dY, const void *dH, const void *H, const vo
  *                  Rows behind the last sequence are left as they were.
  *   k_len          NULL, or (without cu_k) device int32[B]: sequence b has k_len[b] <= max_k keys; what lies behind them is not read
  *   D              head size: a multiple of 8, at most 128
- *   scale          positive and finite, in fp32 as well
+ *   scale          from 2^-100 to 2^127
  *   lse            NULL, or fp32: [B, Hq, max_q], packed [Hq, total_q]
  *   o_rest         NULL, or an array like o (its strides, its alignment) for the backward pass: the rows of tokens that see at most 128
  *                  keys receive what o's rounding took, rounded in turn (the backward pass needs row sums of dO O, whose error would

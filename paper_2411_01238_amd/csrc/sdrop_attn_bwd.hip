@@ -14,16 +14,24 @@ namespace sdrop {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-// Statistics of the rows, two floats each: (lse log2(e) - kPShift, delta kPScale).  dV's P is held as 256 P: over thousands of keys P
-// itself would fall among fp16's smallest numbers, whose steps are coarse.  The factor is part of the two and leaves dS as it is.
-constexpr float kPShift = 8.f, kPScale = 1.f / 256.f;
+// Statistics of the rows, as dK and dV's accumulators begin: -lse / scale, so that exp2(c S) is P, and -delta, so that dP - delta comes out of
+// the matrix cores.  fp16's P is held as 256 P: over thousands of keys P itself would fall among its smallest numbers, whose steps are
+// coarse.  The factor is part of the first and is taken out again.
+template <class T> constexpr float kPShift = 0.f;
+template <> constexpr float kPShift<F16> = 8.f;
+template <class T> constexpr float kPScale = 1.f;
+template <> constexpr float kPScale<F16> = 1.f / 256.f;
 
-// Where the rows of (sequence b, key head hkv) begin in them: on 16 bytes, sequences and heads apart.  A tile of 64 rows is read
-// whole, so the array is that much longer than its last row.
+// Two arrays, and where the rows of (sequence b, key head hkv) begin in each: on 16 bytes, sequences and heads apart.  A tile of 64 rows
+// is read whole, so each is that much longer than its last row.
+__host__ __device__ __forceinline__ int64_t stats_rows(const AttnParams &P)
+{
+    return P.cu_q ? P.Hkv * ((P.total_q * P.G + 4 * P.B + 3) & ~int64_t(3)) : (int64_t)P.B * P.Hkv * ((P.max_rows + 3) & ~3);
+}
 __device__ __forceinline__ int64_t stats_at(const AttnParams &P, const Sequence &s, int b, int hkv)
 {
-    return P.cu_q ? hkv * ((P.total_q * P.G + 2 * P.B + 1) & ~int64_t(1)) + ((s.q0 * P.G + 2 * b) & ~int64_t(1))
-                  : ((int64_t)b * P.Hkv + hkv) * ((P.max_rows + 1) & ~1);
+    return P.cu_q ? hkv * ((P.total_q * P.G + 4 * P.B + 3) & ~int64_t(3)) + ((s.q0 * P.G + 4 * b) & ~int64_t(3))
+                  : ((int64_t)b * P.Hkv + hkv) * ((P.max_rows + 3) & ~3);
 }
 
 template <class T> __device__ __forceinline__ float dot8(uint4 a, uint4 b, float sum)
@@ -91,7 +99,11 @@ __global__ __launch_bounds__(256, HD <= 64 ? 4 : 2) void attn_dq_kernel(AttnPara
     if (live) {
         const float x = P.lse[P.cu_q ? head * P.total_q + s.q0 + i : ((int64_t)b * P.Hq + head) * P.max_q + i];
         if (x != -INFINITY) lse2 = x * kLog2e;
-        if (h == 0 && wk == 0) reinterpret_cast<float2 *>(P.delta)[stats_at(P, s, b, hkv) + r] = make_float2(lse2 - kPShift, delta * kPScale);
+        if (h == 0 && wk == 0) {
+            float *const st = P.delta + stats_at(P, s, b, hkv) + r;
+            st[0] = (kPShift<T> - lse2) / P.c;
+            st[stats_rows(P) + 64] = -delta;
+        }
     }
 
     f32x16 acc[DB];
@@ -180,7 +192,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnParams P)
 {
     constexpr int TQ = 64, TILE = tile_bytes<HD>(TQ), DB = HD / 32, RW = 4 / KW, KEYS = 32 * KW;
     __shared__ __attribute__((aligned(1024))) char lds[4 * TILE + 2 * TQ * 8];
-    float *const st = reinterpret_cast<float *>(lds + 4 * TILE);       // [2][TQ][2]
+    float *const st = reinterpret_cast<float *>(lds + 4 * TILE);       // [2][2][TQ]
     const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), h = lane >> 5;
     int bh, unit;
     place(P, P.tiles, bh, unit);
@@ -221,7 +233,8 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnParams P)
 
     const char *const qb = P.q + (P.cu_q ? 0 : b * P.q_b) + s.q0 * P.q_t + (int64_t)hkv * P.G * P.q_h;
     const char *const gb = P.dout + (P.cu_q ? 0 : b * P.do_b) + s.q0 * P.do_t + (int64_t)hkv * P.G * P.do_h;
-    const char *const stats = reinterpret_cast<const char *>(reinterpret_cast<const float2 *>(P.delta) + stats_at(P, s, b, hkv));
+    const char *const stats = reinterpret_cast<const char *>(P.delta + stats_at(P, s, b, hkv));
+    const int64_t second = (stats_rows(P) + 64) * 4;
     const int nch = P.D / 8;
     // rows of a tile are tokens and heads of the group in turn: each lane works out where its rows lie
     constexpr int ROW_BYTES = 2 * HD, RPI = 1024 / ROW_BYTES, PASSES = TQ / (RPI * 4);
@@ -258,7 +271,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnParams P)
                 }
             }
         }
-        if (threadIdx.x < TQ / 2) dma16_at(stats + (int64_t)t * TQ * 8 + ln * 16, lds + 4 * TILE + buf * TQ * 8);
+        if (threadIdx.x < TQ / 2) dma16_at(stats + (int64_t)t * TQ * 4 + (ln & 15) * 16 + (ln < 16 ? 0 : second), lds + 4 * TILE + buf * TQ * 8);
     };
     if (t0 < t1) request(t0, 0);
     for (int t = t0; t < t1; ++t) {
@@ -277,14 +290,20 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnParams P)
             // (a wavefront at its matrix instructions goes before the one beside it at its exponentials: 2 x 4096, 16 heads of 128, causal
             // 350 -> 332 us)
             __builtin_amdgcn_s_setprio(1);
-            f32x16 sc = zero16(), dp = zero16();
+            f32x16 sc, dp;
+            const float *const stb = st + buf * 2 * TQ + 32 * mb + 4 * h;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32q a4 = *reinterpret_cast<const f32q *>(stb + 8 * g), b4 = *reinterpret_cast<const f32q *>(stb + TQ + 8 * g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { sc[4 * g + e] = a4[e]; dp[4 * g + e] = b4[e]; }
+            }
 #pragma unroll
             for (int kk = 0; kk < HD / 16; ++kk) sc = In<T>::mfma(ra.get(0, kk), kf[kk], sc);
 #pragma unroll
             for (int kk = 0; kk < HD / 16; ++kk) dp = In<T>::mfma(ra.get(TILE, kk), vf[kk], dp);
-            const float *const stb = st + (buf * TQ + 32 * mb + 4 * h) * 2;
             // the operands are read two ahead of the matrix instructions (three would not leave the accumulators their registers)
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 8 + 2, 0);
 #pragma unroll
             for (int i = 0; i < HD / 8 - 2; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -294,14 +313,9 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnParams P)
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32q a4 = *reinterpret_cast<const f32q *>(stb + 16 * g), b4 = *reinterpret_cast<const f32q *>(stb + 16 * g + 4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(sc[4 * g + e] * P.c - (e < 2 ? a4 : b4)[2 * (e & 1)]);
-                    sc[4 * g + e] = p;
-                    dp[4 * g + e] = p * (dp[4 * g + e] * kPScale - (e < 2 ? a4 : b4)[2 * (e & 1) + 1]);
-                }
+            for (int e = 0; e < 16; ++e) {
+                sc[e] = __builtin_amdgcn_exp2f(sc[e] * P.c);
+                dp[e] *= kPScale<T> == 1.f ? sc[e] : sc[e] * kPScale<T>;
             }
             // rows that do not see the key, and rows that do not exist (whose statistics are another's, or none)
             if ((P.causal && see_first < w0 + 31) || rb + 32 > rows) {
@@ -384,7 +398,7 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnParams P)
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
         store_row32<T>(dkp + 64 * d, dk[d], P.scale, P.D - 32 * d, write);
-        store_row32<T>(dvp + 64 * d, dv[d], kPScale, P.D - 32 * d, write);
+        store_row32<T>(dvp + 64 * d, dv[d], kPScale<T>, P.D - 32 * d, write);
     }
 }
 
@@ -427,11 +441,7 @@ template <class T, int HD> int launch_bwd(AttnParams P, hipStream_t st)
     return hip_status(hipGetLastError());
 }
 
-size_t stats_bytes(const AttnParams &P)
-{
-    const size_t rows = P.cu_q ? (size_t)P.Hkv * (((size_t)P.total_q * P.G + 2 * P.B + 1) & ~size_t(1)) : (size_t)P.B * P.Hkv * ((P.max_rows + 1) & ~1);
-    return (rows + 64) * 2 * sizeof(float);
-}
+size_t stats_bytes(const AttnParams &P) { return (size_t)(stats_rows(P) + 64) * 2 * sizeof(float); }
 
 }  // namespace
 }  // namespace sdrop

@@ -433,7 +433,7 @@ int attn_params(const sdrop_attn_t *a, bool backward, AttnParams &P)
     P.g_mul = (uint32_t)(((uint64_t(1) << 32) * ((uint64_t(1) << P.g_shift) - (uint64_t)P.G)) / (uint64_t)P.G + 1);
     P.scale = (float)a->scale;
     P.c = (float)(a->scale * 1.4426950408889634);
-    if (!(P.scale > 0.f && P.c > 0.f && P.c < INFINITY)) return SDROP_EINVAL;       // (beyond what fp32 holds)
+    if (!(P.c >= 0x1p-100f && P.c < INFINITY)) return SDROP_EINVAL;         // (the backward pass divides lse by it)
     P.status = device_status_word();
     return SDROP_OK;
 }
