@@ -109,6 +109,16 @@ __global__ __launch_bounds__(256, HD <= 64 ? 4 : 2) void attn_dq_kernel(AttnPara
     f32x16 acc[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = zero16();
+    // dP's accumulators begin at -delta; heads of 64 have no registers to keep that in, and subtract it
+    constexpr bool BEGIN = HD > 64;
+    f32x16 dp0 = zero16();
+    if constexpr (BEGIN) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            dp0[e] = -delta;
+            asm volatile("" : "+v"(dp0[e]));
+        }
+    }
     const char *kb = P.k + (P.cu_k ? 0 : b * P.k_b) + s.k0 * P.k_t + hkv * P.k_h;
     const char *vb = P.v + (P.cu_k ? 0 : b * P.v_b) + s.k0 * P.v_t + hkv * P.v_h;
     const int nch = P.D / 8;
@@ -134,7 +144,7 @@ __global__ __launch_bounds__(256, HD <= 64 ? 4 : 2) void attn_dq_kernel(AttnPara
         auto block = [&](int mb) __attribute__((always_inline)) {
             const RowOperand<HD, T> ka(kt + mb * row_at<HD>(32)), va(vt + mb * row_at<HD>(32));
             const ColOperand<HD, T> kc(kt + mb * row_at<HD>(32));
-            f32x16 sc = zero16(), dp = zero16();
+            f32x16 sc = zero16(), dp = dp0;
 #pragma unroll
             for (int kk = 0; kk < HD / 16; ++kk) sc = In<T>::mfma(ka.get(0, kk), qf[kk], sc);
 #pragma unroll
@@ -146,7 +156,7 @@ __global__ __launch_bounds__(256, HD <= 64 ? 4 : 2) void attn_dq_kernel(AttnPara
                     if (8 * (e >> 2) + (e & 3) > last) sc[e] = -INFINITY;
             }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sc[e] = __builtin_amdgcn_exp2f(sc[e] * P.c - lse2) * (dp[e] - delta);
+            for (int e = 0; e < 16; ++e) sc[e] = __builtin_amdgcn_exp2f(sc[e] * P.c - lse2) * (BEGIN ? dp[e] : dp[e] - delta);
 #pragma unroll
             for (int ks = 0; ks < 2; ++ks) {
                 const typename In<T>::vec ds = narrow8<T>(sc, ks);
