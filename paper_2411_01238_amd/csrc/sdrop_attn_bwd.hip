@@ -198,7 +198,7 @@ __global__ __launch_bounds__(256, HD <= 64 ? 4 : 2) void attn_dq_kernel(AttnPara
 // KW wavefronts own keys of their own; the 4 / KW wavefronts of the same keys take a tile's blocks of 32 rows in turn and are joined at
 // the end.
 template <class T, int HD, int KW>
-__global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnParams P)
+__global__ __launch_bounds__(256, HD <= 64 ? 3 : 2) void attn_dkv_kernel(AttnParams P)
 {
     constexpr int TQ = 64, TILE = tile_bytes<HD>(TQ), DB = HD / 32, RW = 4 / KW, KEYS = 32 * KW;
     __shared__ __attribute__((aligned(1024))) char lds[4 * TILE + 2 * TQ * 8];
@@ -248,17 +248,29 @@ __global__ __launch_bounds__(256, 2) void attn_dkv_kernel(AttnParams P)
     const int nch = P.D / 8;
     // rows of a tile are tokens and heads of the group in turn: each lane works out where its rows lie
     constexpr int ROW_BYTES = 2 * HD, RPI = 1024 / ROW_BYTES, PASSES = TQ / (RPI * 4);
+    // offsets of a lane's part of a tile (see request)
+    auto offsets = [&](int ln, int &lrow, int &chunk, uint32_t &qo, uint32_t &go) __attribute__((always_inline)) {
+        lrow = RPI * wave + (ln * 16) / ROW_BYTES;
+        chunk = ((ln * 16) % ROW_BYTES >> 4) ^ swz_a<HD>(lrow);
+        const uint32_t tok = lrow >> P.g_shift, g = lrow & (P.G - 1);
+        qo = tok * (uint32_t)P.q_t + g * (uint32_t)P.q_h + chunk * 16;
+        go = tok * (uint32_t)P.do_t + g * (uint32_t)P.do_h + chunk * 16;
+    };
+    int lrow0, chunk0;
+    uint32_t qo0, go0;
+    offsets(lane, lrow0, chunk0, qo0, go0);
     auto request = [&](int t, int buf) __attribute__((always_inline)) {
-        // (made anew for every tile: kept over the loop they are registers that the accumulators need)
-        int ln = lane;
-        asm volatile("" : "+v"(ln));
-        const int lrow = RPI * wave + (ln * 16) / ROW_BYTES, chunk = ((ln * 16) % ROW_BYTES >> 4) ^ swz_a<HD>(lrow);
+        int ln = lane, lrow = lrow0, chunk = chunk0;
+        uint32_t qo = qo0, go = go0;
+        if constexpr (HD > 64) {
+            // (made anew for every tile: kept over the loop they are registers that the accumulators need)
+            asm volatile("" : "+v"(ln));
+            offsets(ln, lrow, chunk, qo, go);
+        }
         char *const dst = lds + buf * 2 * TILE;
         if (P.steady && (t + 1) * TQ <= rows && nch == HD / 8) {
             // every pass has the same heads of the group, tokens further on: 32-bit offsets from addresses that the lanes share
-            const int tok = lrow >> P.g_shift, g = lrow & (P.G - 1), t_tok = t * TQ >> P.g_shift, step = RPI * 4 >> P.g_shift;
-            const uint32_t qo = (uint32_t)tok * (uint32_t)P.q_t + (uint32_t)g * (uint32_t)P.q_h + chunk * 16;
-            const uint32_t go = (uint32_t)tok * (uint32_t)P.do_t + (uint32_t)g * (uint32_t)P.do_h + chunk * 16;
+            const int t_tok = t * TQ >> P.g_shift, step = RPI * 4 >> P.g_shift;
             const char *q_at = qb + t_tok * P.q_t, *g_at = gb + t_tok * P.do_t;
 #pragma unroll
             for (int p = 0; p < PASSES; ++p, q_at += step * P.q_t, g_at += step * P.do_t) {
