@@ -7,6 +7,7 @@
 // tile of rows that walks the keys (it has dO and O of its rows at hand and leaves lse and delta for the other), then dK and dV, a
 // workgroup per tile of keys that walks the rows of all query heads that share them.  Each gradient is summed in registers in
 // a fixed order: no atomics, results repeat bit for bit, at the price of computing S and dP twice (7 products instead of 5).
+// Many sequences of up to 256 keys: one launch, a workgroup per sequence and key head, 5 products.
 #include "attn_common.h"
 #include <math.h>
 
@@ -41,6 +42,11 @@ template <class T> __device__ __forceinline__ float dot8(uint4 a, uint4 b, float
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum += static_cast<float>(x[i]) * static_cast<float>(y[i]);
     return sum;
+}
+
+template <int CTRL> __device__ __forceinline__ float lane_sum(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
 
 // dQ.  As in the forward pass a lane holds keys of one query: S^T = K Q^T, dP^T = V dO^T, dQ^T = K^T dS^T; lse and delta are one number
@@ -424,6 +430,232 @@ __global__ __launch_bounds__(256, HD <= 64 ? 3 : 2) void attn_dkv_kernel(AttnPar
     }
 }
 
+// All three gradients of sequences that one workgroup takes whole: W wavefronts own 32 keys each and walk the rows in tiles of 32, as for
+// dK and dV; their dS also goes to LDS, where the wavefronts whose turn it is multiply it with K into dQ during the next tile.  Five
+// products instead of seven, and one pass over memory (64 x 256 tokens, 8 heads of 128: 268 MB in 86 us, 3.1 TB/s; what bounds it is that the
+// two wavefronts of a SIMD meet at every tile, for LDS holds one workgroup per CU).
+template <class T, int HD, int W>
+__global__ __launch_bounds__(64 * W, 2) void attn_bwd_short_kernel(AttnParams P)
+{
+    constexpr int TQ = 32, KEYS = 32 * W, DB = HD / 32, QT = tile_bytes<HD>(TQ), KT = tile_bytes<HD>(KEYS), ST = tile_bytes<64>(KEYS), TURNS = W / DB;
+    static_assert(W % DB == 0, "whole turns");
+    // K; dS [keys][32 rows of an even tile, 32 of an odd one]; two tiles of Q and dO; two of the rows' statistics
+    __shared__ __attribute__((aligned(1024))) char lds[KT + ST + 4 * QT + 4 * TQ * 4];
+    char *const k_lds = lds, *const s_lds = lds + KT, *const q_lds = s_lds + ST;
+    float *const st = reinterpret_cast<float *>(q_lds + 4 * QT);       // [2][2][TQ]
+    const int lane = threadIdx.x & 63, wave = uni(threadIdx.x >> 6), h = lane >> 5;
+    const int bh = uni(blockIdx.x), b = bh / P.Hkv, hkv = bh - b * P.Hkv;
+    const Sequence s = sequence_of(P, b);
+    if (!s.ok) return;
+    const int out_rows = P.cu_k ? s.Lk : P.max_k, rows = s.Lq * P.G, off = s.Lk - s.Lq, n = (rows + TQ - 1) / TQ, nch = P.D / 8;
+    const int w0 = 32 * wave, key = w0 + (lane & 31);
+    const int first_row = (int)max((int64_t)-1, min((int64_t)(key - off) * P.G, (int64_t)INT_MAX));      // causal: of those that see the key
+    auto see_last = [&](int t) __attribute__((always_inline)) { return P.causal ? uni(token_of(P, min(t * TQ + TQ, rows) - 1)) + off : s.Lk - 1; };
+
+    {
+        TileLoad<HD, KEYS, W> lk;
+        lk.init(P.k_t, wave);
+        lk.issue(P.k + (P.cu_k ? 0 : b * P.k_b) + s.k0 * P.k_t + hkv * P.k_h, P.k_t, k_lds, s.Lk, nch);
+    }
+    typename In<T>::vec vf[HD / 16];
+    {
+        const int64_t at = s.k0 + min(key, max(s.Lk - 1, 0));
+        const char *const vp = P.v + (P.cu_k ? 0 : b * P.v_b) + at * P.v_t + hkv * P.v_h;
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+            const int col = 16 * kk + 8 * h;
+            uint4 y = make_uint4(0, 0, 0, 0);
+            if (key < s.Lk && col < P.D) y = *reinterpret_cast<const uint4 *>(vp + 2 * col);
+            vf[kk] = __builtin_bit_cast(typename In<T>::vec, y);
+        }
+    }
+    const char *const qb = P.q + (P.cu_q ? 0 : b * P.q_b) + s.q0 * P.q_t + (int64_t)hkv * P.G * P.q_h;
+    const char *const gb = P.dout + (P.cu_q ? 0 : b * P.do_b) + s.q0 * P.do_t + (int64_t)hkv * P.G * P.do_h;
+
+    // Q and dO of a tile: pieces of 1 KiB, shared out to the wavefronts
+    constexpr int ROW_BYTES = 2 * HD, RPI = 1024 / ROW_BYTES, PIECES = TQ / RPI;
+    static_assert(2 * PIECES % W == 0, "every wavefront has as many");
+    auto request = [&](int t, int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int p = 0; p < 2 * PIECES / W; ++p) {
+            const int piece = wave + W * p, which = piece / PIECES, i = piece % PIECES, ln = lane_again();
+            const int lrow = RPI * i + (ln * 16) / ROW_BYTES, chunk = ((ln * 16) % ROW_BYTES >> 4) ^ swz_a<HD>(lrow);
+            const char *const base = which ? gb : qb;
+            const int64_t xt = which ? P.do_t : P.q_t, xh = which ? P.do_h : P.q_h;
+            char *const at = q_lds + (2 * buf + which) * QT + i * 1040;
+            if (P.steady && (t + 1) * TQ <= rows && nch == HD / 8) {
+                const uint32_t tok = lrow >> P.g_shift, g = lrow & (P.G - 1);
+                dma16(base + (t * TQ >> P.g_shift) * xt, tok * (uint32_t)xt + g * (uint32_t)xh + chunk * 16, at);
+            } else {
+                const int rr = t * TQ + lrow;
+                if (rr < rows && chunk < nch) {
+                    const int tok = token_of(P, rr), g = rr - tok * P.G;
+                    dma16_at(base + tok * xt + g * xh + chunk * 16, at);
+                } else {
+                    *reinterpret_cast<uint4 *>(at + ln * 16) = make_uint4(0, 0, 0, 0);
+                }
+            }
+        }
+    };
+
+    // The rows' statistics: 16 bytes of a row per thread, asked for before and added up behind the work on the tile before
+    constexpr int CH = HD / 8;
+    const bool adds = threadIdx.x < TQ * CH && (int)threadIdx.x % CH < nch;
+    uint4 xg, xo, xr;
+    float xl;
+    const char *g_at, *o_at;
+    const float *l_at;
+    auto find = [&](int t) __attribute__((always_inline)) {
+        const int r = min(t * TQ + (int)threadIdx.x / CH, rows - 1), i = token_of(P, r), g = r - i * P.G, head = hkv * P.G + g, chunk = threadIdx.x % CH;
+        g_at = gb + i * P.do_t + g * P.do_h + chunk * 16;
+        o_at = P.o + (P.cu_q ? 0 : b * P.o_b) + (s.q0 + i) * P.o_t + head * P.o_h + chunk * 16;
+        l_at = P.lse + (P.cu_q ? head * P.total_q + s.q0 + i : ((int64_t)b * P.Hq + head) * P.max_q + i);
+    };
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+        const int r = t * TQ + (int)threadIdx.x / CH;
+        xg = xo = xr = make_uint4(0, 0, 0, 0);
+        xl = -INFINITY;
+        if (t == 0 || !P.steady) {
+            find(t);
+        } else {
+            // (whole tokens further on, the same head)
+            const int step = TQ >> P.g_shift;
+            g_at += step * P.do_t;
+            o_at += step * P.o_t;
+            l_at += step;
+        }
+        if (adds && r < rows) {
+            xg = *reinterpret_cast<const uint4 *>(g_at);
+            xo = *reinterpret_cast<const uint4 *>(o_at);
+            if (P.rest && (P.causal ? min(s.Lk - 1, token_of(P, r) + off) : s.Lk - 1) < kFewKeys) xr = *reinterpret_cast<const uint4 *>(o_at + (P.rest - P.o));
+            xl = *l_at;
+        }
+    };
+    auto statistics = [&](int buf) __attribute__((always_inline)) {
+        float delta = dot8<T>(xg, xr, dot8<T>(xg, xo, 0.f));
+        delta += lane_sum<0xB1>(delta);
+        delta += lane_sum<0x4E>(delta);
+        delta += lane_sum<0x141>(delta);
+        if constexpr (CH == 16) delta += lane_sum<0x140>(delta);
+        if (threadIdx.x < TQ * CH && threadIdx.x % CH == 0) {
+            float *const at = st + buf * 2 * TQ + threadIdx.x / CH;
+            // (a row that saw no key, or that does not exist: P = 0)
+            at[0] = xl == -INFINITY ? -INFINITY : (kPShift<T> - xl * kLog2e) / P.c;
+            at[TQ] = -delta;
+        }
+    };
+
+    f32x16 dk[DB], dv[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zero16();
+
+    auto rows_and_keys = [&](int t) __attribute__((always_inline)) {
+        const int buf = t & 1, rb = t * TQ;
+        const int see_first = P.causal ? uni(token_of(P, rb)) + off : s.Lk;
+        if (see_last(t) < w0 || w0 >= s.Lk) return;
+        const RowOperand<HD, T> ra(q_lds + buf * 2 * QT), ka(k_lds + row_at<HD>(32) * wave);
+        const ColOperand<HD, T> ca(q_lds + buf * 2 * QT);
+        f32x16 sc, dp;
+        const float *const stb = st + buf * 2 * TQ + 4 * h;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const f32q a4 = *reinterpret_cast<const f32q *>(stb + 8 * g), b4 = *reinterpret_cast<const f32q *>(stb + TQ + 8 * g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { sc[4 * g + e] = a4[e]; dp[4 * g + e] = b4[e]; }
+        }
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) sc = In<T>::mfma(ra.get(0, kk), ka.get(0, kk), sc);
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) dp = In<T>::mfma(ra.get(QT, kk), vf[kk], dp);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            sc[e] = __builtin_amdgcn_exp2f(sc[e] * P.c);
+            dp[e] *= kPScale<T> == 1.f ? sc[e] : sc[e] * kPScale<T>;
+        }
+        // rows that do not see the key, and keys that do not exist
+        if ((P.causal && see_first < w0 + 31) || w0 + 32 > s.Lk) {
+            const int from = key >= s.Lk ? TQ : P.causal ? first_row - rb - 4 * h : 0;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (8 * (e >> 2) + (e & 3) < from) sc[e] = dp[e] = 0.f;
+        }
+        typename In<T>::vec pn[2], dn[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) { pn[ks] = narrow8<T>(sc, ks); dn[ks] = narrow8<T>(dp, ks); }
+        char *const to = s_lds + row_at<64>(32) * wave + row_at<64>(lane & 31) + 8 * h;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const uint4 x = __builtin_bit_cast(uint4, dn[ks]);
+            *reinterpret_cast<uint2 *>(to + (((4 * buf + 2 * ks) ^ swz_a<64>(lane & 31)) << 4)) = make_uint2(x.x, x.y);
+            *reinterpret_cast<uint2 *>(to + (((4 * buf + 2 * ks + 1) ^ swz_a<64>(lane & 31)) << 4)) = make_uint2(x.z, x.w);
+        }
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+            for (int d = 0; d < DB; ++d) dv[d] = In<T>::mfma(ca.get(QT, d, ks), pn[ks], dv[d]);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) dk[d] = In<T>::mfma(ca.get(0, d, ks), dn[ks], dk[d]);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int i = 0; i < 4 * DB - 2; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // dQ^T = K^T dS^T of a tile whose turn is this wavefront's, 32 columns
+    auto queries = [&](int t) __attribute__((always_inline)) {
+        if (wave / DB != t % TURNS) return;
+        const int d = wave % DB, steps = (min(s.Lk, see_last(t) + 1) + 15) / 16;
+        const ColOperand<HD, T> kc(k_lds);
+        const ColOperand<64, T> sa(s_lds);
+        f32x16 acc = zero16();
+        int ks = 0;
+        for (; ks + 4 <= steps; ks += 4) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) acc = In<T>::mfma(kc.get(0, d, ks + u), sa.get(0, t & 1, ks + u), acc);
+        }
+        for (; ks < steps; ++ks) acc = In<T>::mfma(kc.get(0, d, ks), sa.get(0, t & 1, ks), acc);
+        const int r = t * TQ + (lane_again() & 31), i = token_of(P, min(r, rows - 1)), head = hkv * P.G + (min(r, rows - 1) - i * P.G);
+        char *const dst = P.dq + (P.cu_q ? 0 : b * P.dq_b) + (s.q0 + i) * P.dq_t + head * P.dq_h;
+        store_row32<T>(dst + 64 * d, acc, P.scale, P.D - 32 * d, r < rows);
+    };
+
+    if (n > 0) {
+        request(0, 0);
+        fetch(0);
+        statistics(0);
+    }
+    for (int t = 0; t < n; ++t) {
+        landed();
+        if (t + 1 < n) {
+            request(t + 1, (t + 1) & 1);
+            fetch(t + 1);
+        }
+        if (t > 0) queries(t - 1);
+        rows_and_keys(t);
+        if (t + 1 < n) statistics((t + 1) & 1);
+    }
+    landed();
+    if (n > 0) queries(n - 1);
+
+    const int mine = w0 + (lane_again() & 31);
+    if (mine >= s.Lk) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zero16();
+    }
+    const bool write = mine < out_rows;
+    char *const dkp = P.dk + (P.cu_k ? 0 : b * P.dk_b) + (s.k0 + mine) * P.dk_t + hkv * P.dk_h;
+    char *const dvp = P.dv + (P.cu_k ? 0 : b * P.dv_b) + (s.k0 + mine) * P.dv_t + hkv * P.dv_h;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) {
+        store_row32<T>(dkp + 64 * d, dk[d], P.scale, P.D - 32 * d, write);
+        store_row32<T>(dvp + 64 * d, dv[d], kPScale<T>, P.D - 32 * d, write);
+    }
+}
+
 // dK and dV on tiles of 64 keys, two wavefronts sharing out the rows of the same keys, instead of 128: where the larger tiles leave the
 // chip half empty, or where they are all at work at once and the longest of them (the first keys under a causal mask, the longest of
 // packed sequences) is what the call waits for.  Small tiles read each row twice as often.  us, 128 -> 64: 4096 tokens, 8 heads of
@@ -445,8 +677,24 @@ bool few_rows(const AttnParams &P)
     return (P.max_k >= 512 && full <= cus) || (P.D <= 64 && P.causal && P.max_k >= 2048 && full <= 4 * cus);
 }
 
+// One workgroup per sequence and key head, all three gradients in one pass over memory, instead of dQ and then dK and dV: up to 256 keys (what
+// LDS holds), with heads enough for a quarter of the CUs.  us, two launches -> one: 64 x 256 tokens, 8 heads of 128, no mask 111 -> 86, causal
+// 101 -> 76; 32 x 128, causal 32 -> 21; 8 x 256, 32 heads, 8 of keys, causal 103 -> 90; 128 x 197, 12 heads of 64 137 -> 135; 64 x 128, no
+// mask 50 -> 31; but 4 x 256, 8 heads of 128 29 -> 33.
+bool whole_sequences(const AttnParams &P)
+{
+    const int64_t heads = (int64_t)P.B * P.Hkv;
+    return P.max_k <= 256 && 4 * heads >= cu_count() && heads <= (1 << 22);
+}
+
 template <class T, int HD> int launch_bwd(AttnParams P, hipStream_t st)
 {
+    if (whole_sequences(P)) {
+        const dim3 grid((unsigned)((int64_t)P.B * P.Hkv));
+        if (HD <= 64 && P.max_k <= 128) hipLaunchKernelGGL((attn_bwd_short_kernel<T, 64, 4>), grid, dim3(256), 0, st, P);
+        else hipLaunchKernelGGL((attn_bwd_short_kernel<T, HD, 8>), grid, dim3(512), 0, st, P);
+        return hip_status(hipGetLastError());
+    }
     const int rows = few_rows(P) ? 64 : 128;
     P.tiles = (P.max_rows + rows - 1) / rows;
     const dim3 row_grid((unsigned)((int64_t)P.B * P.Hkv * P.tiles));

@@ -99,6 +99,73 @@ def test_dense_forward_and_backward(B, Tq, Tk, Hq, Hkv, D, causal, dtype):
     assert sdrop.status() == 0
 
 
+# heads enough that a workgroup takes a sequence's gradients whole: up to 256 keys, group sizes that divide 16 and others
+SHORT = [
+    (16, 197, 197, 4, 4, 64, False), (64, 33, 33, 2, 1, 128, True), (22, 100, 256, 9, 3, 72, True), (64, 1, 9, 1, 1, 8, True), (13, 40, 31, 25, 5, 40, False),
+    (16, 70, 130, 16, 4, 128, True), (8, 90, 60, 32, 8, 96, True), (64, 64, 128, 1, 1, 64, False), (64, 129, 256, 1, 1, 128, False), (2, 3, 2, 64, 32, 16, True),
+]
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hkv,D,causal", SHORT)
+def test_many_short_sequences(B, Tq, Tk, Hq, Hkv, D, causal, dtype):
+    test_dense_forward_and_backward(B, Tq, Tk, Hq, Hkv, D, causal, dtype)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 2, 64), (6, 2, 128)])
+def test_many_short_packed_sequences(Hq, Hkv, D, dtype):
+    print("short packed", Hq, Hkv, D, dtype, flush=True)
+    td = DT[dtype]
+    g = np.random.default_rng(5)
+    lq = [0, 1, 32, 33, 150, 0] + [int(n) for n in g.integers(0, 90, 34)]
+    lk = [9, 0, 32, 1, 250, 0] + [int(n) for n in g.integers(0, 90, 34)]
+    cq, ck = (torch.tensor(np.concatenate([[0], np.cumsum(l)]), dtype=torch.int32, device="cuda") for l in (lq, lk))
+    nq, nk = sum(lq) + 5, sum(lk) + 5
+    q, do, k, v = _randn((nq, Hq, D), td, 1), _randn((nq, Hq, D), td, 4), _randn((nk, Hkv, D), td, 2), _randn((nk, Hkv, D), td, 3)
+    for t in (q, do, k, v):
+        t[-5:] = float("nan")
+    out = [torch.full_like(t, 7.0) for t in (q, k, v)]
+    kw = dict(cu_q=cq, cu_k=ck, max_q=150, max_k=256)
+    o, lse, rest = sdrop.sdrop_attn(q, k, v, True, need_rest=True, **kw)
+    sdrop.sdrop_attn_bwd(do, q, k, v, o, lse, True, rest=rest, out_dq=out[0], out_dk=out[1], out_dv=out[2], **kw)
+    assert all(bool((t[-5:] == 7.0).all()) for t in out)
+    for b in range(len(lq)):
+        a, z = slice(int(cq[b]), int(cq[b + 1])), slice(int(ck[b]), int(ck[b + 1]))
+        if lk[b] == 0:
+            assert not out[0][a].any()
+        if lq[b] == 0:
+            assert not out[1][z].any() and not out[2][z].any()
+        if lq[b] and lk[b]:
+            _check(q[a], k[z], v[z], do[a], True, td, [o[a], out[0][a], out[1][z], out[2][z]], lse[:, a], "seq %d" % b)
+    assert sdrop.status() == 0
+
+
+def test_short_sequences_padded_and_as_slices_of_one_tensor():
+    td = torch.bfloat16
+    B, T, H, D = 16, 120, 4, 64
+    q, k, v, do = (_randn((B, T, H, D), td, i) for i in range(4))
+    lens = [T, 0, 1, 33, 64, 119] + [7 * b for b in range(6, B)]
+    for b, n in enumerate(lens):
+        k[b, n:], v[b, n:] = float("nan"), float("inf")
+    kl = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    o, lse, rest = sdrop.sdrop_attn(q, k, v, True, k_len=kl, need_rest=True)
+    dq, dk, dv = sdrop.sdrop_attn_bwd(do, q, k, v, o, lse, True, k_len=kl, rest=rest)
+    for b, n in enumerate(lens):
+        if n:
+            _check(q[b], k[b, :n], v[b, :n], do[b], True, td, (o[b], dq[b], dk[b, :n], dv[b, :n]), lse[b], "b=%d n=%d" % (b, n))
+        assert not dk[b, n:].any() and not dv[b, n:].any() and (n or not dq[b].any())
+    # a fused projection's slices, and heads before tokens: the same bits
+    x = _randn((B, T, 3 * H, D), td, 9).requires_grad_()
+    parts = [t.detach().contiguous().requires_grad_() for t in (x[:, :, :H], x[:, :, H:2 * H], x[:, :, 2 * H:])]
+    turned = [t.detach().transpose(1, 2).contiguous().transpose(1, 2).requires_grad_() for t in parts]
+    gx, = torch.autograd.grad(tr.qkv_attention(x, H), x, do)
+    gp = torch.autograd.grad(tr.attention(*parts), parts, do)
+    gt = torch.autograd.grad(tr.attention(*turned), turned, do)
+    assert torch.equal(gx, torch.cat(gp, dim=2)) and all(torch.equal(a, b) for a, b in zip(gp, gt))
+    assert sdrop.status() == 0
+
+
 FEW = [(1, 1, 5000, 1, 1, 128, True), (3, 1, 777, 8, 2, 128, True), (2, 4, 3000, 8, 1, 64, True), (1, 8, 9000, 3, 1, 96, False), (64, 1, 130, 4, 4, 64, True)]
 
 
