@@ -658,13 +658,16 @@ __global__ __launch_bounds__(64 * W, 2) void attn_bwd_short_kernel(AttnParams P)
 
 // dK and dV on tiles of 64 keys, two wavefronts sharing out the rows of the same keys, instead of 128: where the larger tiles leave the
 // chip half empty, or where they are all at work at once and the longest of them (the first keys under a causal mask, the longest of
-// packed sequences) is what the call waits for.  Small tiles read each row twice as often.  us, 128 -> 64: 4096 tokens, 8 heads of
-// 128, no mask 210 -> 196, causal 172 -> 125; 2 x 2048, 16 heads of 64, causal 68 -> 55; but 2 x 4096, 16 heads of 128, causal 349 -> 430;
-// 4 x 1024, 16 heads of 128, causal 60 -> 66; 32 x 128, 8 heads of 128, causal 14.0 -> 15.4.
+// packed sequences) is what the call waits for.  Small tiles read each row twice as often.  us of the backward pass, 128 -> 64: 4096 tokens,
+// 8 heads of 128, no mask 250 -> 239, causal 207 -> 168; 2 x 2048, 16 heads of 64, causal 93 -> 82; 40 packed sequences of up to 1024 tokens,
+// 16 heads of 64, 4 of keys 243 -> 230; but 2 x 4096, 16 heads of 128, causal 471 -> 482; 4 x 1024 93 -> 94; 100 packed sequences of up to
+// 2048 tokens, 16 heads of 64, 4 of keys 1407 -> 1494.
 bool few_key_tiles(const AttnParams &P)
 {
-    const int64_t keys = P.cu_k ? P.total_k : (int64_t)P.B * P.max_k, tiles = keys / 128 * P.Hkv;
-    return P.max_k >= 1024 && tiles <= (P.causal || P.cu_k ? 2 : 1) * (int64_t)cu_count() && !(P.causal && !P.cu_k && P.max_k < 2048 && tiles > cu_count());
+    const int64_t keys = P.cu_k ? P.total_k : (int64_t)P.B * P.max_k, tiles = keys / 128 * P.Hkv, cus = cu_count();
+    if (P.max_k < (P.cu_k ? 512 : 1024)) return false;
+    if (P.cu_k) return tiles <= (P.D <= 64 ? 4 : 2) * cus;
+    return tiles <= (P.causal && P.max_k >= 2048 ? 2 : 1) * cus;
 }
 
 // dQ on 64 rows a workgroup, two wavefronts sharing out the keys of the same rows, instead of 128.  us, 128 -> 64: 2048 tokens, 8
