@@ -332,6 +332,29 @@ def test_offsets_beyond_32_bits():
     _check(q[B - 1, :, :1], kv[B - 1, :, 127:], kv[B - 1, :, 127:], None, False, td, (o2[0],), None, "last head")
 
 
+@pytest.mark.parametrize("B,T", [(1, 300), (64, 100)])
+def test_gradients_of_heads_far_apart(B, T):
+    # the two query heads of a key head 2 GiB apart: the same bits as side by side
+    td = torch.bfloat16
+    D, far = 64, 1 << 30
+    q, do = _randn((B, T, 2, D), td, 1), _randn((B, T, 2, D), td, 2)
+    k, v = _randn((B, T, 1, D), td, 3), _randn((B, T, 1, D), td, 4)
+    apart = []
+    for t in (q, do, q):
+        x = torch.empty(far + B * T * D, dtype=td, device="cuda").as_strided(t.shape, (T * D, D, far, 1))
+        x.copy_(t)
+        apart.append(x)
+    o, lse, rest = sdrop.sdrop_attn(q, k, v, True, need_rest=True)
+    want = sdrop.sdrop_attn_bwd(do, q, k, v, o, lse, True, rest=rest)
+    o2, lse2, rest2 = sdrop.sdrop_attn(apart[0], k, v, True, need_rest=True)
+    got = sdrop.sdrop_attn_bwd(apart[1], apart[0], k, v, o2, lse2, True, rest=rest2, out_dq=apart[2])
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    for b in {0, B - 1}:
+        _check(q[b], k[b], v[b], do[b], True, td, [t[b] for t in (o,) + want], lse[b], "b=%d" % b)
+
+
 def test_results_repeat_on_another_stream_and_in_a_graph():
     td = torch.bfloat16
     q, do, k, v = _randn((2, 300, 4, 128), td, 1), _randn((2, 300, 4, 128), td, 2), _randn((2, 300, 2, 128), td, 3), _randn((2, 300, 2, 128), td, 4)
