@@ -582,7 +582,8 @@ int sdrop_layer_norm_bwd(const void *dY, const void *dH, const void *H, const vo
  *
  * Query head h reads key / value head h / (Hq / Hkv).  Token i of Lq sees all Lk keys of its sequence or, causal, the keys
  * j <= i + Lk - Lq (the last token sees every key: new tokens behind a cache).  A token that sees no key has O = 0, lse = -inf.
- * Products run on the matrix cores; scores, statistics and sums are fp32, P is rounded to `dtype` for the second product.  A key
+ * Products run on the matrix cores; scores, statistics and sums are fp32, P is rounded to `dtype` for the second product (what that takes from
+ * keys that have a large part of their row is added).  A key
  * that a token does not see has P = 0 whatever its score; its v still takes part as 0 times v (as in the formula), so it has to
  * be finite, except behind k_len and between packed sequences, where nothing is read.
  *
@@ -597,9 +598,8 @@ int sdrop_layer_norm_bwd(const void *dY, const void *dH, const void *H, const vo
  *   D              head size: a multiple of 8, at most 128
  *   scale          from 2^-100 to 2^127
  *   lse            NULL, or fp32: [B, Hq, max_q], packed [Hq, total_q]
- *   o_rest         NULL, or an array like o (its strides, its alignment) for the backward pass: the rows of tokens that see at most 128
- *                  keys receive what o's rounding took, rounded in turn (the backward pass needs row sums of dO O, whose error would
- *                  otherwise be that of a rounded O); the other rows are not written, and not read there
+ *   o_rest         NULL, or an array like o (its strides, its alignment) for the backward pass: it receives what o's rounding took,
+ *                  rounded in turn (the backward pass needs row sums of dO O, whose error would otherwise be that of a rounded O)
  *   ws, ws_bytes   sdrop_attn_workspace_bytes(a) bytes (partial results where few queries share many keys out to the whole
  *                  chip; may be 0), 16-byte aligned
  *

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256, HD <= 64 ? 4 : 2) void attn_dq_kernel(AttnPara
                 x = *reinterpret_cast<const uint4 *>(qp + 2 * col);
                 g = *reinterpret_cast<const uint4 *>(gp + 2 * col);
                 o = *reinterpret_cast<const uint4 *>(P.o + at + 2 * col);
-                if (P.rest && lim < kFewKeys) rest = *reinterpret_cast<const uint4 *>(P.rest + at + 2 * col);
+                if (P.rest) rest = *reinterpret_cast<const uint4 *>(P.rest + at + 2 * col);
             }
             qf[kk] = __builtin_bit_cast(typename In<T>::vec, x);
             gf[kk] = __builtin_bit_cast(typename In<T>::vec, g);
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_bwd_short_kernel(AttnParams P)
         if (adds && r < rows) {
             xg = *reinterpret_cast<const uint4 *>(g_at);
             xo = *reinterpret_cast<const uint4 *>(o_at);
-            if (P.rest && (P.causal ? min(s.Lk - 1, token_of(P, r) + off) : s.Lk - 1) < kFewKeys) xr = *reinterpret_cast<const uint4 *>(o_at + (P.rest - P.o));
+            if (P.rest) xr = *reinterpret_cast<const uint4 *>(o_at + (P.rest - P.o));
             xl = *l_at;
         }
     };

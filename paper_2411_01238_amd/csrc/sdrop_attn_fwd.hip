@@ -35,7 +35,6 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? (HD <= 64 ? 4 : 2) : 1
     const int off = s.Lk - s.Lq;                    // causal: token i sees keys up to i + off
     const int r_last = min(R0 + 32 * QW, rows) - 1;
     const int k_end = P.causal ? min(s.Lk, token_of(P, r_last) + off + 1) : s.Lk;
-    const bool whole_p = (P.causal ? token_of(P, R0) + off + 1 : s.Lk) <= kFewKeys;         // (of this tile's first row)
     // this workgroup's part of the key tiles
     const int n_tiles = k_end > 0 ? (k_end + TKV - 1) / TKV : 0, per = (n_tiles + P.splits - 1) / P.splits;
     const int t0 = min(split * per, n_tiles), t1 = min(t0 + per, n_tiles);
@@ -64,6 +63,8 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? (HD <= 64 ? 4 : 2) : 1
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[d] = zero16();
     float m = -INFINITY, l = 0.f;           // running maximum (of S before the scale) and this lane's part of the sum
+    const float rc = __builtin_amdgcn_rcpf(P.c);
+    float large_from = -INFINITY;           // scores above this have a large share (kLargeShare), or are 2^8 beyond the maximum
 
     // 32 * MB keys from kv0 on, whose K and V lie at kt and vt
     auto compute_keys = [&](int kv0, const char *kt, const char *vt) __attribute__((always_inline)) {
@@ -103,8 +104,10 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? (HD <= 64 ? 4 : 2) : 1
 #pragma unroll
             for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[mb][e]);
         mx = join_halves(mx, [](float a, float b2) { return fmaxf(a, b2); });
+        const bool large = mx > large_from;
+        const uint64_t any_large = __ballot(large);
         // O and the sum are rescaled only when a maximum has grown by more than 2^8 in P: until then P stays below 256
-        if (__any(mx > m && (mx - m) * P.c > 8.f)) {
+        if (any_large && __any(mx > m && (mx - m) * P.c > 8.f)) {
             const float mn = fmaxf(m, mx);
             const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * P.c);
             l *= f;
@@ -122,6 +125,7 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? (HD <= 64 ? 4 : 2) : 1
                 sc[mb][e] = __builtin_amdgcn_exp2f(sc[mb][e] * P.c - mc);
                 l += sc[mb][e];
             }
+        large_from = m + fminf(__builtin_amdgcn_logf(kLargeShare * l), 8.f) * rc;
         const ColOperand<HD, T> va(vt);
         if constexpr (HD <= 64 && MB == 2) __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
@@ -142,10 +146,12 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? (HD <= 64 ? 4 : 2) : 1
             __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_s_setprio(0);
-        if (whole_p) {
+        if (any_large) {
+            // (nothing is added to other rows: a row's result does not depend on those beside it)
+            const uint32_t mask = large ? ~0u : 0u;
 #pragma unroll
             for (int ks = 0; ks < 2 * MB; ++ks) {
-                const typename In<T>::vec p = narrow8_rest<T>(sc[ks >> 1], ks & 1);
+                const typename In<T>::vec p = narrow8_rest<T>(sc[ks >> 1], ks & 1, mask);
 #pragma unroll
                 for (int d = 0; d < DB; ++d) o[d] = In<T>::mfma(va.get(0, d, ks), p, o[d]);
             }
@@ -269,7 +275,7 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? (HD <= 64 ? 4 : 2) : 1
     const int64_t at = (P.cu_q ? 0 : b * P.o_b) + (s.q0 + i_out) * P.o_t + head_out * P.o_h;
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-        store_row32<T>(P.out + at + 64 * d, o[d], inv, P.D - 32 * d, live_out, P.out_rest && whole_p ? P.out_rest + at + 64 * d : nullptr, (P.causal ? i_out + off : s.Lk - 1) < kFewKeys);
+        store_row32<T>(P.out + at + 64 * d, o[d], inv, P.D - 32 * d, live_out, P.out_rest ? P.out_rest + at + 64 * d : nullptr);
     }
 }
 
@@ -326,7 +332,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnParams P)
             const e2 x = {static_cast<E>(a0 * inv), static_cast<E>(a1 * inv)};
             const int64_t at = (P.cu_q ? 0 : b * P.o_b) + (s.q0 + i) * P.o_t + head * P.o_h + 4 * lane;
             *reinterpret_cast<e2 *>(P.out + at) = x;
-            if (P.out_rest && (P.causal ? min(s.Lk, i + s.Lk - s.Lq + 1) : s.Lk) <= kFewKeys) {
+            if (P.out_rest) {
                 const e2 y = {static_cast<E>(a0 * inv - static_cast<float>(x[0])), static_cast<E>(a1 * inv - static_cast<float>(x[1]))};
                 *reinterpret_cast<e2 *>(P.out_rest + at) = y;
             }

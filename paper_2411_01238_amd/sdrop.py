@@ -915,7 +915,7 @@ def sdrop_attn(q, k, v, causal=False, scale=None, cu_q=None, cu_k=None, max_q=No
                ws=None):
     """O = softmax(scale q k^T) v per head (scale: D ** -0.5 if not given); returns (O, lse), lse the fp32 log-sum-exp of the scores
     that the backward pass needs: [B, Hq, Tq], packed [Hq, tokens] (None with need_lse=False).  need_rest: (O, lse, rest), rest what
-    O's rounding took for tokens that see at most 128 keys (other rows hold nothing); the backward pass is the more exact for it.
+    O's rounding took; the backward pass is the more exact for it.
 
     q [B, Tq, Hq, D], k and v [B, Tk, Hkv, D] in fp16 or bf16, Hq a multiple of Hkv, D a multiple of 8 up to 128, any strides that keep
     16-byte alignment and contiguous D.  causal: token i sees keys up to i + Lk - Lq.  cu_q / cu_k: int32 offsets [B + 1] of packed

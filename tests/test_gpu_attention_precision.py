@@ -1,0 +1,107 @@
+"""Rounding errors of attention's gradients (arxiv 2411.01238, Section 4.2's models) where the usual inputs do not show them: scores so
+far apart that a few keys carry a row, and gradients whose products with P are far smaller than fp16's usual numbers.
+
+Tolerances are on norms of the errors.  A rounding is off by at most e = eps / 2 of the value and evenly spread over half a step, so the mean
+of its square is at most e^2 / 3, and roundings have signs of their own: in sums the squares add.  What a gradient may have:
+    dS                one rounding per value: e^2 / 3 of dS^2
+    delta             row sums of dO O.  P is rounded for O, but for keys that have more than half of their row: squared, e^2 / 3 of the sum
+                      of the others' (P dP)^2, which reaches every key of the row by P.  O's second part is rounded: e^2 of O
+    fp32              sums of 128 products: 128 roundings of 2^-24, below 2^-20 of the magnitudes; P by the error of its score, below 2^-13
+                      for scores below 2^7, which reaches dS and delta as a rounding does
+    the result        e^2 / 3 of its square, or half a step of fp16's smallest numbers (2^-25), squared, / 3
+The mantissas of usual values are larger than 1: the mean square of a rounding is 0.18 e^2 for them, so that 0.74 of these tolerances is what
+an implementation with exactly these errors shows.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2411_01238_amd import sdrop
+from _util import f64
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def head_bounds(q, k, v, do, scale, causal, e):
+    """One head in float64: ((dq, dk, dv), and for dq and dk the allowed norm of the error without the result's own rounding)."""
+    s = scale * (q @ k.T)
+    if causal:
+        i, j = np.arange(q.shape[0])[:, None], np.arange(k.shape[0])[None, :]
+        s = np.where(j <= i + k.shape[0] - q.shape[0], s, -np.inf)
+    p = np.exp(s - s.max(axis=1, keepdims=True))
+    p /= p.sum(axis=1, keepdims=True)
+    o, dp = p @ v, do @ v.T
+    delta = (do * o).sum(axis=1, keepdims=True)
+    ds = p * (dp - delta)
+    grads = scale * (ds @ k), scale * (ds.T @ q), p.T @ do
+    small = 2.0 ** -13
+    arith = 2.0 ** -20 * p * (np.abs(do) @ np.abs(v).T + (np.abs(do) * np.abs(o)).sum(axis=1, keepdims=True))
+    rounded = e ** 2 / 3 + small ** 2
+    row = rounded * (np.where(p > 0.5, ds, p * dp) ** 2).sum(axis=1) + e ** 4 * ((do * o) ** 2).sum(axis=1)         # delta's error, squared
+    own = rounded * ds ** 2 + arith ** 2
+    k2, q2 = (k ** 2).sum(axis=1), (q ** 2).sum(axis=1)
+    bq = scale * np.sqrt((own @ k2).sum() + (row * ((p @ k) ** 2).sum(axis=1)).sum())
+    bk = scale * np.sqrt((own.T @ q2).sum() + (row * (p ** 2).sum(axis=1) * q2).sum())
+    return grads, (bq, bk)
+
+
+def check_heads(q, k, v, do, got, causal, dtype, what, scale=None, some=None):
+    """got: (dq, dk, dv), [B, T, H, D] each; one key head per query head."""
+    e, tiny = torch.finfo(dtype).eps / 2, 2.0 ** -25 if dtype == torch.float16 else 0.0
+    scale = q.shape[-1] ** -0.5 if scale is None else scale
+    for b, h in (some or [(b, h) for b in range(q.shape[0]) for h in range(q.shape[2])]):
+        qd, kd, vd, gd = (f64(t[b, :, h]) for t in (q, k, v, do))
+        want, allow = head_bounds(qd, kd, vd, gd, scale, causal, e)
+        for name, g, w, a in zip(("dq", "dk"), got, want, allow):
+            err = np.linalg.norm(f64(g[b, :, h]) - w)
+            bound = np.sqrt(a ** 2 + e ** 2 / 3 * (w ** 2).sum() + tiny ** 2 / 3 * w.size)
+            assert err <= bound, "%s, b=%d h=%d, %s: error %.3g of its bound (%.3g of the gradient)" % (what, b, h, name, err / bound, err / np.linalg.norm(w))
+
+
+def randn(shape, dtype, seed, std=1.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64) * std).to(dtype).cuda()
+
+
+def gradients(q, k, v, do, causal, scale=None, **kw):
+    o, lse, rest = sdrop.sdrop_attn(q, k, v, causal, scale, need_rest=True, **kw)
+    return sdrop.sdrop_attn_bwd(do, q, k, v, o, lse, causal, scale, rest=rest, **kw)
+
+
+# two launches on tiles of 64 and of 128, sequences that one workgroup takes whole, few rows over parts of the keys
+SHAPES = [(1, 1024, 1024, 2, 128, True), (2, 700, 700, 3, 64, False), (4, 1000, 1000, 16, 64, False), (32, 250, 250, 4, 128, True), (64, 200, 256, 2, 64, False), (1, 16, 4096, 2, 128, True)]
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("std", [1, 3, 10])
+@pytest.mark.parametrize("B,Tq,Tk,H,D,causal", SHAPES)
+def test_gradients_where_few_keys_carry_a_row(B, Tq, Tk, H, D, causal, std, dtype):
+    print("scores of deviation", std, B, Tq, Tk, H, D, causal, dtype, flush=True)
+    td = DT[dtype]
+    q, k = randn((B, Tq, H, D), td, 1, std ** 0.5), randn((B, Tk, H, D), td, 2, std ** 0.5)
+    v, do = randn((B, Tk, H, D), td, 3), randn((B, Tq, H, D), td, 4)
+    check_heads(q, k, v, do, gradients(q, k, v, do, causal), causal, td, "deviation %d" % std, some=[(0, 0), (B - 1, H - 1), (B // 2, H // 2)])
+    assert sdrop.status() == 0
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Tq", [1, 200])
+def test_many_keys_of_a_small_share_each(Tq, D):
+    # fp16: one key takes half, 16000 others, each of them among fp16's smallest numbers as a share of it, the rest.  A rounding there is
+    # at most 2^-25 of the largest P
+    td = torch.float16
+    T = 16000
+    q = torch.zeros((1, Tq, 1, D), dtype=td, device="cuda")
+    q[..., 0] = 1.0
+    k, v = randn((1, T, 1, D), td, 1), randn((1, T, 1, D), td, 2)
+    k[..., 0] = torch.linspace(-10.0, -9.5, T, device="cuda").to(td)[None, :, None]
+    k[0, 777, 0, 0] = 0.0
+    o, lse = sdrop.sdrop_attn(q, k, v, False, 1.0)
+    sc, vd = f64(k)[0, :, 0, 0], f64(v)[0, :, 0]
+    p = np.exp(sc)
+    want = p @ vd / p.sum()
+    e = torch.finfo(td).eps / 2
+    bound = e * np.abs(want) + ((np.maximum(e * p, 2.0 ** -25) + 2.0 ** -18 * p) / p.sum()) @ np.abs(vd)
+    assert (np.abs(f64(o)[0, :, 0] - want) <= bound).all()
+    assert (np.abs(f64(lse)[0, 0] - np.log(p.sum())) <= 2.0 ** -13).all()
