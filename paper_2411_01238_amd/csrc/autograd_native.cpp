@@ -47,7 +47,8 @@ int type_code(const Tensor &t, const char *what)
     }
 }
 
-// t [.., N] as M rows, ld elements apart: a matrix with contiguous rows as it is, any other tensor that lies in one piece, else a copy.
+// t [.., N] as M rows, ld elements apart (at most 2^24): a matrix with contiguous rows as it is, any other tensor that lies in one piece, else
+// a copy.
 struct Rows {
     Tensor t;
     int64_t M, N, ld;
@@ -57,7 +58,7 @@ struct Rows {
         N = x.size(-1);
         M = N ? x.numel() / N : 0;
         ld = N;
-        if (x.dim() == 2 && (N == 1 || x.stride(1) == 1) && (M <= 1 || x.stride(0) >= N)) {
+        if (x.dim() == 2 && (N == 1 || x.stride(1) == 1) && (M <= 1 || (x.stride(0) >= N && x.stride(0) <= int64_t(1) << 24))) {
             if (M > 1) ld = x.stride(0);
         } else if (!x.is_contiguous()) {
             t = x.contiguous();
@@ -255,12 +256,15 @@ struct DropoutAddNorm : torch::autograd::Function<DropoutAddNorm> {
 
 // ---- attention ----
 
-// What the kernels take in place (contiguous heads, 16-byte steps and addresses), else a copy.
+// What the kernels take in place (contiguous heads, 16-byte steps and addresses, tokens at most 2^24 elements apart), else a copy: of a tensor
+// in one piece too, which may begin anywhere (a gradient that comes back through a concatenation).
 Tensor in_place(const Tensor &t)
 {
-    bool ok = t.is_cuda() && t.dim() >= 3 && (t.stride(-1) == 1 || t.size(-1) == 1) && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0;
-    for (int64_t d = 0; ok && d < t.dim() - 1; ++d) ok = t.size(d) == 1 || (t.stride(d) > 0 && t.stride(d) % 8 == 0);
-    return ok ? t : t.contiguous();
+    if (!t.is_cuda() || t.dim() < 3) return t;          // (refused where the call is described)
+    bool ok = (t.stride(-1) == 1 || t.size(-1) == 1) && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0;
+    for (int64_t d = 0; ok && d < t.dim() - 1; ++d)
+        ok = t.size(d) == 1 || (t.stride(d) > 0 && t.stride(d) % 8 == 0 && t.stride(d) <= int64_t(1) << (d == t.dim() - 3 ? 24 : 50));
+    return ok ? t : t.clone(at::MemoryFormat::Contiguous);
 }
 
 void strides(const Tensor &t, int64_t &b, int64_t &tok, int64_t &h)

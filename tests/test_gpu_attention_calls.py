@@ -1,0 +1,63 @@
+"""Calls of the transformer operators (arxiv 2411.01238, Section 4.2's models) as programs come to make them: tensors that begin or lie anywhere,
+batches with nothing in them, lengths that do not fit."""
+import pytest
+import torch
+
+from paper_2411_01238_amd import sdrop
+from paper_2411_01238_amd import transformer as tr
+
+pytestmark = pytest.mark.gpu
+
+
+def randn(shape, dtype, seed, std=1.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed), dtype=torch.float64) * std).to(dtype).cuda()
+
+
+def placed(t, offset):
+    """t's values in one piece, `offset` elements into a buffer."""
+    x = torch.empty(t.numel() + offset, dtype=t.dtype, device=t.device)[offset:].view(t.shape)
+    return x.copy_(t)
+
+
+@pytest.mark.parametrize("offset", [1, 3, 4])
+def test_tensors_in_one_piece_that_begin_anywhere(offset):
+    td = torch.bfloat16
+    q, do, k, v = (randn((2, 70, h, 64), td, i) for i, h in enumerate((4, 4, 2, 2)))
+
+    def run(f):
+        leaves = [f(t).detach().requires_grad_() for t in (q, k, v)]
+        y = tr.attention(*leaves, causal=True)
+        x = f(torch.cat((q, k, v), dim=2)).detach().requires_grad_()
+        z = tr.qkv_attention(x, 2, causal=True)
+        assert torch.equal(y, z)
+        with torch.no_grad():
+            assert torch.equal(tr.attention(*(f(t) for t in (q, k, v)), causal=True), y)
+        return [y.detach()] + list(torch.autograd.grad(y, leaves, f(do))) + list(torch.autograd.grad(z, x, f(do)))
+
+    for a, b in zip(run(lambda t: placed(t, offset)), run(lambda t: t)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("before", [1, 3, 8])
+def test_gradients_that_come_back_through_a_concatenation(before):
+    td = torch.float16
+    x = randn((2, 50, 6, 64), td, 1).requires_grad_()
+    first, g = randn((before,), td, 2), randn((before + 2 * 50 * 2 * 64,), td, 3)
+    forms = (lambda: tr.qkv_attention(x, 2, causal=True), lambda: tr.attention(x[:, :, :2], x[:, :, 2:4], x[:, :, 4:], causal=True))
+    for f in forms:
+        y = f()
+        joined, = torch.autograd.grad(torch.cat((first, y.flatten())), x, g)
+        direct, = torch.autograd.grad(f(), x, g[before:].clone().view(y.shape))
+        assert torch.equal(joined, direct)
+
+
+def test_tokens_and_rows_far_apart_are_copied():
+    td, far = torch.bfloat16, (1 << 24) + 8
+    room = torch.empty(3 * far, dtype=td, device="cuda")
+    t = randn((1, 3, 2, 64), td, 1)
+    q = room.as_strided((1, 3, 2, 64), (0, far, 64, 1)).copy_(t)
+    assert torch.equal(tr.attention(q, t, t), tr.attention(t, t, t))
+    rows = room.as_strided((3, 128), (far, 1)).copy_(t.view(3, 128))
+    w = randn((128,), td, 2)
+    assert torch.equal(tr.layer_norm(rows, w), tr.layer_norm(t.view(3, 128), w))
+    assert torch.equal(tr.dropout(rows, 0.5, 1, residual=rows), tr.dropout(t.view(3, 128), 0.5, 1, residual=t.view(3, 128)))
