@@ -319,14 +319,16 @@ sdrop_attn_t describe(const Tensor &q, const Tensor &k, const Tensor &v, const A
     return d;
 }
 
-// (rows behind the last packed sequence belong to no one: they are 0)
-Tensor like(const Tensor &t, bool packed) { return packed ? torch::zeros(t.sizes(), t.options()) : torch::empty(t.sizes(), t.options()); }
+// A result like t.  With offsets or lengths not every row is written: those behind the last packed sequence, and those of a sequence whose
+// values do not fit the call, are 0.
+bool some_left(const AttnArgs &a) { return a.cu_q || a.cu_k || a.k_len; }
+Tensor like(const Tensor &t, const AttnArgs &a) { return some_left(a) ? torch::zeros(t.sizes(), t.options()) : torch::empty(t.sizes(), t.options()); }
 
 // o; for_backward: also lse and what o's rounding took
 Tensor attn_forward(const Tensor &q, const Tensor &k, const Tensor &v, const AttnArgs &a, bool for_backward, Tensor &lse, Tensor &rest)
 {
     sdrop_attn_t d = describe(q, k, v, a);
-    Tensor o = like(q, a.cu_q.has_value());
+    Tensor o = like(q, a);
     strides(o, d.o_b, d.o_t, d.o_h);
     if (for_backward) {
         const auto f = q.options().dtype(torch::kFloat);
@@ -395,9 +397,9 @@ struct Attention : torch::autograd::Function<Attention> {
         Tensor dq, dk, dv;
         {
             at::AutoDispatchBelowADInplaceOrView guard;
-            dq = like(s[0], a.cu_q.has_value());
-            dk = like(s[1], a.cu_k.has_value());
-            dv = like(s[2], a.cu_k.has_value());
+            dq = like(s[0], a);
+            dk = like(s[1], a);
+            dv = like(s[2], a);
             attn_backward(g[0], s[0], s[1], s[2], s[3], s[4], s[5], a, dq, dk, dv);
         }
         return once({dq, dk, dv, Tensor()}, joined(g, s));
@@ -432,7 +434,7 @@ struct QkvAttention : torch::autograd::Function<QkvAttention> {
         Tensor d;
         {
             at::AutoDispatchBelowADInplaceOrView guard;
-            d = like(s[0], a.cu_q.has_value());
+            d = like(s[0], a);
             auto part = [&](const Tensor &t, int i) { return i == 0 ? t.narrow(-2, 0, hq) : t.narrow(-2, hq + (i - 1) * hkv, hkv); };
             attn_backward(g[0], part(s[0], 0), part(s[0], 1), part(s[0], 2), s[1], s[2], s[3], a, part(d, 0), part(d, 1), part(d, 2));
         }

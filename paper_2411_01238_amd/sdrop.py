@@ -911,6 +911,12 @@ def _attn_desc(q, k, v, causal, scale, cu_q, cu_k, max_q, max_k, k_len):
     return a, pq, pk, pv
 
 
+def _result(t, some_left):
+    """A new result like t.  With offsets or lengths not every row is written: those behind the last packed sequence, and those of a sequence
+    whose values do not fit the call, are 0."""
+    return (torch.zeros if some_left else torch.empty)(t.shape, dtype=t.dtype, device=t.device)
+
+
 def sdrop_attn(q, k, v, causal=False, scale=None, cu_q=None, cu_k=None, max_q=None, max_k=None, k_len=None, out=None, need_lse=True, need_rest=False,
                ws=None):
     """O = softmax(scale q k^T) v per head (scale: D ** -0.5 if not given); returns (O, lse), lse the fp32 log-sum-exp of the scores
@@ -919,16 +925,19 @@ def sdrop_attn(q, k, v, causal=False, scale=None, cu_q=None, cu_k=None, max_q=No
 
     q [B, Tq, Hq, D], k and v [B, Tk, Hkv, D] in fp16 or bf16, Hq a multiple of Hkv, D a multiple of 8 up to 128, any strides that keep
     16-byte alignment and contiguous D.  causal: token i sees keys up to i + Lk - Lq.  cu_q / cu_k: int32 offsets [B + 1] of packed
-    sequences in [tokens, heads, D], with max_q / max_k bounding their lengths.  k_len: int32 [B], how many of the Tk keys there are."""
+    sequences in [tokens, heads, D], with max_q / max_k bounding their lengths.  k_len: int32 [B], how many of the Tk keys there are.
+    A sequence whose offsets or length do not fit is left out (see status): in new results its O is 0, its lse -inf, its gradients 0."""
     a, pq, pk, pv = _attn_desc(q, k, v, causal, scale, cu_q, cu_k, max_q, max_k, k_len)
+    some_left = any(t is not None for t in (cu_q, cu_k, k_len))
     if out is None:
-        # (rows behind the last packed sequence are not written)
-        out = (torch.empty if cu_q is None else torch.zeros)(q.shape, dtype=q.dtype, device=q.device)
+        out = _result(q, some_left)
     po, (a.o_b, a.o_t, a.o_h) = _heads(out, "out", q.shape[:-2], a.Hq, a.D, q.dtype)
     rest = torch.empty_strided(out.shape, out.stride(), dtype=q.dtype, device=q.device) if need_rest else None
     lse = None
     if need_lse:
         lse = torch.empty((a.B, a.Hq, a.max_q) if cu_q is None else (a.Hq, a.total_q), dtype=torch.float32, device=q.device)
+        if some_left:
+            lse.fill_(float("-inf"))
     _on_current_device(out, ws)
     L = lib()
     ref = ctypes.byref(a)
@@ -947,10 +956,10 @@ def sdrop_attn_bwd(dO, q, k, v, O, lse, causal=False, scale=None, cu_q=None, cu_
     lead_q, lead_k = q.shape[:-2], k.shape[:-2]
     if lse.dtype != torch.float32 or tuple(lse.shape) != ((a.B, a.Hq, a.max_q) if cu_q is None else (a.Hq, a.total_q)):
         raise ValueError("lse must be the fp32 tensor that sdrop_attn returned")
-    new = lambda t, cu: (torch.empty if cu is None else torch.zeros)(t.shape, dtype=q.dtype, device=q.device)     # noqa: E731
-    out_dq = new(q, cu_q) if out_dq is None else out_dq
-    out_dk = new(k, cu_k) if out_dk is None else out_dk
-    out_dv = new(k, cu_k) if out_dv is None else out_dv
+    some_left = any(t is not None for t in (cu_q, cu_k, k_len))
+    out_dq = _result(q, some_left) if out_dq is None else out_dq
+    out_dk = _result(k, some_left) if out_dk is None else out_dk
+    out_dv = _result(v, some_left) if out_dv is None else out_dv
     pg, (a.do_b, a.do_t, a.do_h) = _heads(dO, "dO", lead_q, a.Hq, a.D, q.dtype)
     po, so = _heads(O, "O", lead_q, a.Hq, a.D, q.dtype)
     a.o_b, a.o_t, a.o_h = so

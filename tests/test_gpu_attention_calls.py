@@ -61,3 +61,57 @@ def test_tokens_and_rows_far_apart_are_copied():
     w = randn((128,), td, 2)
     assert torch.equal(tr.layer_norm(rows, w), tr.layer_norm(t.view(3, 128), w))
     assert torch.equal(tr.dropout(rows, 0.5, 1, residual=rows), tr.dropout(t.view(3, 128), 0.5, 1, residual=t.view(3, 128)))
+
+
+def dirty():
+    """What the next results are likely to lie on: memory full of NaN."""
+    for n in (1, 4):
+        x = torch.full((n << 18,), float("nan"), dtype=torch.float32, device="cuda")
+        del x
+
+
+def test_sequences_whose_lengths_do_not_fit_are_zero_in_new_results():
+    td = torch.bfloat16
+    B, T, H, D = 3, 50, 2, 64
+    q, do = randn((B, T, H, D), td, 1), randn((B, T, H, D), td, 2)
+    kl = torch.tensor([20, -1, T + 1], dtype=torch.int32, device="cuda")
+    good = torch.tensor([20], dtype=torch.int32, device="cuda")
+    ref = sdrop.sdrop_attn(q[:1], q[:1], q[:1], True, k_len=good, need_rest=True)
+    want = ref[:2] + sdrop.sdrop_attn_bwd(do[:1], q[:1], q[:1], q[:1], ref[0], ref[1], True, k_len=good, rest=ref[2])
+    assert sdrop.status() == 0
+
+    def check(got, empty):
+        for x, w, e in zip(got, want, empty):
+            assert torch.equal(x[:1], w) and bool((x[1:] == e).all())
+
+    dirty()
+    o, lse, rest = sdrop.sdrop_attn(q, q, q, True, k_len=kl, need_rest=True)
+    dirty()
+    check((o, lse) + sdrop.sdrop_attn_bwd(do, q, q, q, o, lse, True, k_len=kl, rest=rest), (0, float("-inf"), 0, 0, 0))
+    assert sdrop.status() == sdrop.STATUS_BAD_LENGTHS
+    leaves = [q.detach().requires_grad_() for _ in range(3)]
+    dirty()
+    y = tr.attention(*leaves, causal=True, k_len=kl)
+    dirty()
+    g = torch.autograd.grad(y, leaves, do)
+    check((y.detach(),), (0,))
+    for x, w in zip(g, want[2:]):
+        assert torch.equal(x[:1], w) and not x[1:].any()
+    x = torch.cat((q, q, q), dim=2).requires_grad_()
+    dirty()
+    y = tr.qkv_attention(x, H, causal=True, k_len=kl)
+    dirty()
+    g, = torch.autograd.grad(y, x, do)
+    assert torch.equal(y[:1], want[0]) and not y[1:].any() and torch.equal(g[:1], torch.cat(want[2:], dim=2)) and not g[1:].any()
+    # packed queries over dense keys: offsets that do not fit leave the keys' gradients at 0 too
+    cu = torch.tensor([0, T, T - 1, 2 * T], dtype=torch.int32, device="cuda")
+    p = q.view(B * T, H, D)
+    dirty()
+    o, lse = sdrop.sdrop_attn(p, q, q, cu_q=cu, max_q=T)
+    dirty()
+    dk, dv = sdrop.sdrop_attn_bwd(do.view(B * T, H, D), p, q, q, o, lse, cu_q=cu, max_q=T)[1:]
+    for t in (o[:T], dk[:1], dv[:1]):
+        assert bool(t.any())
+    for t in (o[2 * T:], dk[1:], dv[1:]):
+        assert not t.any()
+    assert bool((lse[:, 2 * T:] == float("-inf")).all()) and sdrop.status() == sdrop.STATUS_BAD_LENGTHS
