@@ -408,8 +408,9 @@ int attn_params(const sdrop_attn_t *a, bool backward, AttnParams &P)
         if (!stride_ok(strides[i][0], wide) || !stride_ok(strides[i][1], token) || !stride_ok(strides[i][2], wide)) return SDROP_ESHAPE;
         // an output's elements have places of their own
         const bool keys = i >= 6;
+        const int64_t tokens = keys ? (a->cu_k ? a->total_k : a->max_k) : a->cu_q ? a->total_q : a->max_q;
         if ((backward ? i >= 5 : i == 3) && ((strides[i][0] == 0 && a->B > 1 && !(keys ? a->cu_k : a->cu_q)) ||
-            (strides[i][1] == 0 && (keys ? a->max_k : a->max_q) > 1) || (strides[i][2] == 0 && (keys ? a->Hkv : a->Hq) > 1))) return SDROP_ESHAPE;
+            (strides[i][1] == 0 && tokens > 1) || (strides[i][2] == 0 && (keys ? a->Hkv : a->Hq) > 1))) return SDROP_ESHAPE;
     }
     P = AttnParams();
     P.q_b = 2 * a->q_b; P.q_t = 2 * a->q_t; P.q_h = 2 * a->q_h;

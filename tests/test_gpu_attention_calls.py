@@ -115,3 +115,24 @@ def test_sequences_whose_lengths_do_not_fit_are_zero_in_new_results():
     for t in (o[2 * T:], dk[1:], dv[1:]):
         assert not t.any()
     assert bool((lse[:, 2 * T:] == float("-inf")).all()) and sdrop.status() == sdrop.STATUS_BAD_LENGTHS
+
+
+def test_packed_batches_of_one_token():
+    # [tokens, heads, D] with one token in all, under a bound that is larger: the other sequences are empty
+    td = torch.float16
+    cu = torch.tensor([0, 0, 1, 1], dtype=torch.int32, device="cuda")
+    q, k, v, do = (randn((1, 2, 64), td, i) for i in range(4))
+    kw = dict(cu_q=cu, cu_k=cu, max_q=100, max_k=100)
+    o, lse, rest = sdrop.sdrop_attn(q, k, v, True, need_rest=True, **kw)
+    dq, dk, dv = sdrop.sdrop_attn_bwd(do, q, k, v, o, lse, True, rest=rest, **kw)
+    # P = 1: dP and delta are the same sum of 64 products, in fp32 and in orders of their own; each is off by at most 64 roundings of 2^-24
+    # of the sum of the magnitudes (and delta's second part by less), so that dS is below 2^-17 of that sum
+    dS = 2.0 ** -17 * float((do.float() * v.float()).abs().sum(-1).max())
+    most = [dS * 64 ** -0.5 * float(t.abs().max()) + 2.0 ** -25 for t in (k, q)]
+    assert torch.equal(o, v) and torch.equal(dv, do) and float(dq.abs().max()) <= most[0] and float(dk.abs().max()) <= most[1]
+    assert torch.allclose(lse[:, 0], (q.float() * k.float()).sum(-1)[0] / 8, atol=1e-4)
+    x = torch.cat((q, k, v), dim=1).requires_grad_()
+    y = tr.qkv_attention(x, 2, causal=True, cu=cu, max_len=100)
+    g, = torch.autograd.grad(y, x, do)
+    assert torch.equal(y, v) and torch.equal(g, torch.cat((dq, dk, dv), dim=1))
+    assert sdrop.status() == 0
