@@ -33,8 +33,9 @@ def head_bounds(q, k, v, do, scale, causal, e):
     if causal:
         i, j = np.arange(q.shape[0])[:, None], np.arange(k.shape[0])[None, :]
         s = np.where(j <= i + k.shape[0] - q.shape[0], s, -np.inf)
-    p = np.exp(s - s.max(axis=1, keepdims=True))
-    p /= p.sum(axis=1, keepdims=True)
+    top = s.max(axis=1, keepdims=True)
+    p = np.exp(s - np.where(np.isfinite(top), top, 0.0))
+    p /= np.maximum(p.sum(axis=1, keepdims=True), 1e-300)           # (a row that sees no key has P = 0)
     o, dp = p @ v, do @ v.T
     delta = (do * o).sum(axis=1, keepdims=True)
     ds = p * (dp - delta)
