@@ -280,6 +280,7 @@ struct AttnArgs {
     double scale;               // 0: D ** -0.5
     OptTensor cu_q, cu_k, k_len;
     int64_t max_q, max_k;
+    bool train = false;         // a graph is wanted of this call (inside a node's forward pass gradients are off)
 };
 
 // The description of a call on [B, T, H, D] or packed [tokens, H, D] tensors.
@@ -378,13 +379,12 @@ Tensor or_none(const OptTensor &t) { return t ? *t : Tensor(); }
 struct Attention : torch::autograd::Function<Attention> {
     static Tensor forward(AutogradContext *ctx, const Tensor &q0, const Tensor &k0, const Tensor &v0, const AttnArgs &a)
     {
-        const bool train = q0.requires_grad() || k0.requires_grad() || v0.requires_grad();
         at::AutoDispatchBelowADInplaceOrView guard;
         const c10::DeviceGuard on(q0.device());
         const Tensor q = in_place(q0), k = in_place(k0), v = in_place(v0);
         Tensor lse, rest;
-        Tensor o = attn_forward(q, k, v, a, train, lse, rest);
-        if (train) {
+        Tensor o = attn_forward(q, k, v, a, a.train, lse, rest);
+        if (a.train) {
             ctx->save_for_backward({q, k, v, o, lse, rest, or_none(a.cu_q), or_none(a.cu_k), or_none(a.k_len)});
             keep(ctx, a);
         }
@@ -411,15 +411,14 @@ struct Attention : torch::autograd::Function<Attention> {
 struct QkvAttention : torch::autograd::Function<QkvAttention> {
     static Tensor forward(AutogradContext *ctx, const Tensor &qkv0, int64_t hkv, const AttnArgs &a)
     {
-        const bool train = qkv0.requires_grad();
         at::AutoDispatchBelowADInplaceOrView guard;
         const c10::DeviceGuard on(qkv0.device());
         require(qkv0.is_cuda() && (qkv0.dim() == 3 || qkv0.dim() == 4) && hkv >= 1 && qkv0.size(-2) > 2 * hkv, "qkv is a GPU tensor [.., Hq + 2 Hkv, D]");
         const Tensor qkv = in_place(qkv0);
         const int64_t hq = qkv.size(-2) - 2 * hkv;
         Tensor lse, rest;
-        Tensor o = attn_forward(qkv.narrow(-2, 0, hq), qkv.narrow(-2, hq, hkv), qkv.narrow(-2, hq + hkv, hkv), a, train, lse, rest);
-        if (train) {
+        Tensor o = attn_forward(qkv.narrow(-2, 0, hq), qkv.narrow(-2, hq, hkv), qkv.narrow(-2, hq + hkv, hkv), a, a.train, lse, rest);
+        if (a.train) {
             ctx->save_for_backward({qkv, o, lse, rest, or_none(a.cu_q), or_none(a.k_len)});
             keep(ctx, a);
             ctx->saved_data["hkv"] = hkv;
@@ -441,13 +440,6 @@ struct QkvAttention : torch::autograd::Function<QkvAttention> {
         return once({d, Tensor(), Tensor()}, joined(g, s));
     }
 };
-
-Tensor no_graph_attention(const Tensor &q0, const Tensor &k0, const Tensor &v0, const AttnArgs &a)
-{
-    const c10::DeviceGuard on(q0.device());
-    Tensor lse, rest;
-    return attn_forward(in_place(q0), in_place(k0), in_place(v0), a, false, lse, rest);
-}
 
 }  // namespace
 
@@ -472,11 +464,11 @@ PYBIND11_MODULE(_native, m)
     });
     m.def("attention", [](const Tensor &q, const Tensor &k, const Tensor &v, bool causal, double scale, const OptTensor &cu_q, const OptTensor &cu_k,
                           int64_t max_q, int64_t max_k, const OptTensor &k_len) {
-        const AttnArgs a{causal, scale, cu_q, cu_k, k_len, max_q, max_k};
-        if (!at::GradMode::is_enabled()) return no_graph_attention(q, k, v, a);
-        return Attention::apply(q, k, v, a);
+        const bool train = at::GradMode::is_enabled() && (q.requires_grad() || k.requires_grad() || v.requires_grad());
+        return Attention::apply(q, k, v, AttnArgs{causal, scale, cu_q, cu_k, k_len, max_q, max_k, train});
     });
     m.def("qkv_attention", [](const Tensor &qkv, int64_t hkv, bool causal, double scale, const OptTensor &cu, int64_t max_len, const OptTensor &k_len) {
-        return QkvAttention::apply(qkv, hkv, AttnArgs{causal, scale, cu, cu, k_len, max_len, max_len});
+        const bool train = at::GradMode::is_enabled() && qkv.requires_grad();
+        return QkvAttention::apply(qkv, hkv, AttnArgs{causal, scale, cu, cu, k_len, max_len, max_len, train});
     });
 }

@@ -136,3 +136,31 @@ def test_packed_batches_of_one_token():
     g, = torch.autograd.grad(y, x, do)
     assert torch.equal(y, v) and torch.equal(g, torch.cat((dq, dk, dv), dim=1))
     assert sdrop.status() == 0
+
+
+def test_forward_mode_tangents_are_refused_with_gradients_off_too():
+    # (a tangent that is dropped is a wrong derivative)
+    import torch.autograd.forward_ad as fwAD
+    x = randn((1, 20, 6, 64), torch.float16, 1)
+    for f in (lambda t: tr.attention(t[:, :, :2], x[:, :, 2:4], x[:, :, 4:]), lambda t: tr.qkv_attention(t, 2)):
+        for grad in (True, False):
+            with torch.set_grad_enabled(grad), fwAD.dual_level():
+                with pytest.raises(RuntimeError):
+                    f(fwAD.make_dual(x, x))
+    assert sdrop.status() == 0
+
+
+def test_with_gradients_off_nothing_is_kept_for_them():
+    # the same bits, and no more memory than the result's, from inputs that ask for gradients
+    x = randn((4, 512, 24, 128), torch.bfloat16, 1).requires_grad_()
+    forms = (lambda: tr.qkv_attention(x, 8, causal=True), lambda: tr.attention(x[:, :, :8], x[:, :, 8:16], x[:, :, 16:], causal=True))
+    want = [f().detach() for f in forms]
+    for f, w in zip(forms, want):
+        with torch.no_grad():
+            f()
+            torch.cuda.synchronize()
+            before = torch.cuda.memory_allocated()
+            torch.cuda.reset_peak_memory_stats()
+            y = f()
+            assert torch.cuda.max_memory_allocated() - before == y.numel() * 2
+        assert not y.requires_grad and torch.equal(y, w)
