@@ -88,10 +88,17 @@ variable_list joined(variable_list a, const variable_list &b)
 
 uint64_t bits(const c10::IValue &v) { return (uint64_t)v.toInt(); }
 
+// (The C ABI's sizes are positive.  Tensors with nothing in them have results with nothing in them, as torch's operators do; other arguments are
+// checked all the same.)
 Tensor drop(const Rows &x, const Rows *r, double p, uint64_t seed, uint64_t stream, int &rc)
 {
     Tensor y = torch::empty(x.t.sizes(), x.t.options());
-    rc = sdrop_dropout(x.ptr(), r ? r->ptr() : nullptr, y.data_ptr(), x.M, x.N, p, seed, stream, type_code(x.t, "sdrop_dropout"), x.ld,
+    const int dtype = type_code(x.t, "sdrop_dropout");
+    if (!x.t.numel()) {
+        rc = p >= 0.0 && p <= 1.0 ? SDROP_OK : SDROP_EINVAL;
+        return y;
+    }
+    rc = sdrop_dropout(x.ptr(), r ? r->ptr() : nullptr, y.data_ptr(), x.M, x.N, p, seed, stream, dtype, x.ld,
                        r ? r->ld : 0, 0, stream_of(x.t));
     return y;
 }
@@ -146,6 +153,10 @@ void norm_forward(const Rows &x, const Rows *r, const Tensor &w, const OptTensor
     y = torch::empty(x.t.sizes(), x.t.options());
     if (r || p != 0.0) h = torch::empty(x.t.sizes(), x.t.options());
     stats = torch::empty({2, x.M}, x.t.options().dtype(torch::kFloat));
+    if (!x.t.numel()) {
+        type_code(x.t, "sdrop_layer_norm");
+        return check(p >= 0.0 && p <= 1.0 && eps >= 0.0 && eps < INFINITY ? SDROP_OK : SDROP_EINVAL, "sdrop_layer_norm");
+    }
     float *const s = stats.data_ptr<float>();
     check(sdrop_layer_norm(x.ptr(), r ? r->ptr() : nullptr, w.data_ptr(), b ? b->data_ptr() : nullptr, h.defined() ? h.data_ptr() : nullptr,
                            y.data_ptr(), s, s + x.M, x.M, x.N, eps, p, seed, stream, type_code(x.t, "sdrop_layer_norm"),
@@ -163,18 +174,20 @@ void norm_backward(const Tensor &gy, const Tensor &gh, const Tensor &h, const Te
     Tensor dr, dx, dg, db, ws;
     if (need_r || (need_x && !drops)) dr = torch::empty(gy.sizes(), gy.options());
     if (need_x && drops) dx = torch::empty(gy.sizes(), gy.options());
-    if (need_w) dg = torch::empty(w.sizes(), w.options());
-    if (need_b) db = torch::empty(w.sizes(), w.options());
+    const bool none = !gy.numel();
+    if (need_w) dg = none ? torch::zeros(w.sizes(), w.options()) : torch::empty(w.sizes(), w.options());
+    if (need_b) db = none ? torch::zeros(w.sizes(), w.options()) : torch::empty(w.sizes(), w.options());
     size_t need = 0;
-    if (need_w || need_b) {
+    if (!none && (need_w || need_b)) {
         need = sdrop_layer_norm_bwd_workspace_bytes(dy.M, dy.N);
         ws = torch::empty({(int64_t)need}, w.options().dtype(torch::kByte));
     }
     auto at = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
     const float *const s = stats.data_ptr<float>();
-    check_backward(sdrop_layer_norm_bwd(dy.ptr(), dh ? dh->ptr() : nullptr, hs.ptr(), w.data_ptr(), s, s + dy.M, at(dr), at(dx), at(dg), at(db),
-                                        dy.M, dy.N, p, seed, stream, type_code(gy, "sdrop_layer_norm_bwd"), type_code(w, "sdrop_layer_norm_bwd"),
-                                        dy.ld, dh ? dh->ld : 0, hs.ld, 0, 0, at(ws), need, stream_of(gy)), "sdrop_layer_norm_bwd");
+    if (!none)
+        check_backward(sdrop_layer_norm_bwd(dy.ptr(), dh ? dh->ptr() : nullptr, hs.ptr(), w.data_ptr(), s, s + dy.M, at(dr), at(dx), at(dg), at(db),
+                                            dy.M, dy.N, p, seed, stream, type_code(gy, "sdrop_layer_norm_bwd"), type_code(w, "sdrop_layer_norm_bwd"),
+                                            dy.ld, dh ? dh->ld : 0, hs.ld, 0, 0, at(ws), need, stream_of(gy)), "sdrop_layer_norm_bwd");
     out[0] = drops ? dx : need_x ? dr : Tensor();
     out[1] = need_r ? dr : Tensor();
     out[2] = dg;
@@ -325,6 +338,22 @@ sdrop_attn_t describe(const Tensor &q, const Tensor &k, const Tensor &v, const A
 bool some_left(const AttnArgs &a) { return a.cu_q || a.cu_k || a.k_len; }
 Tensor like(const Tensor &t, const AttnArgs &a) { return some_left(a) ? torch::zeros(t.sizes(), t.options()) : torch::empty(t.sizes(), t.options()); }
 
+// No queries, no keys or no sequences: there is nothing to launch, and what the description says of the heads is checked here.
+bool nothing(const Tensor &q, const Tensor &k, const sdrop_attn_t &d)
+{
+    if (q.numel() && k.numel() && d.B) return false;
+    sdrop_attn_t one = {};
+    one.B = one.max_q = one.max_k = 1;
+    one.Hq = d.Hq;
+    one.Hkv = d.Hkv;
+    one.o_h = one.do_h = one.dq_h = one.dk_h = one.dv_h = one.D = d.D;
+    one.scale = d.scale;
+    one.causal = d.causal;
+    one.dtype = d.dtype;
+    check(sdrop_attn_bwd_workspace_bytes(&one) ? SDROP_OK : SDROP_ESHAPE, "sdrop_attn");
+    return true;
+}
+
 // o; for_backward: also lse and what o's rounding took
 Tensor attn_forward(const Tensor &q, const Tensor &k, const Tensor &v, const AttnArgs &a, bool for_backward, Tensor &lse, Tensor &rest)
 {
@@ -336,6 +365,7 @@ Tensor attn_forward(const Tensor &q, const Tensor &k, const Tensor &v, const Att
         lse = a.cu_q ? torch::empty({d.Hq, d.total_q}, f) : torch::empty({d.B, d.Hq, d.max_q}, f);
         rest = torch::empty(q.sizes(), q.options());
     }
+    if (nothing(q, k, d)) return o.zero_();
     const size_t need = sdrop_attn_workspace_bytes(&d);
     Tensor ws;
     if (need) ws = torch::empty({(int64_t)need}, q.options().dtype(torch::kByte));
@@ -350,6 +380,10 @@ void attn_backward(const Tensor &grad, const Tensor &q, const Tensor &k, const T
 {
     const Tensor g = in_place(grad);
     sdrop_attn_t d = describe(q, k, v, a);
+    if (nothing(q, k, d)) {
+        for (const Tensor &t : {dq, dk, dv}) t.zero_();
+        return;
+    }
     strides(o, d.o_b, d.o_t, d.o_h);
     strides(g, d.do_b, d.do_t, d.do_h);
     strides(dq, d.dq_b, d.dq_t, d.dq_h);

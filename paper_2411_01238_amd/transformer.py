@@ -1,6 +1,7 @@
 """What a transformer block (arxiv 2411.01238, Section 4.2) is made of besides its linear layers, as differentiable functions and
 modules: element dropout, layer norm, dropout + residual add + layer norm in one pass, attention.  Everything runs in libsdrop's
-kernels; the autograd nodes around them are in csrc/autograd_native.cpp.  Each can be differentiated once.
+kernels; the autograd nodes around them are in csrc/autograd_native.cpp.  Each can be differentiated once.  Tensors with nothing in them give
+results with nothing in them (attention over no keys: 0).
 
 The dropout's mask is a function of a seed and a stream number (`rng_stream`: one per call, e.g. a step counter) and is never
 stored: the backward pass draws it again.  A captured graph replays the mask of the numbers it was captured with; a module that is run

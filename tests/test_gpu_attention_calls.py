@@ -164,3 +164,50 @@ def test_with_gradients_off_nothing_is_kept_for_them():
             y = f()
             assert torch.cuda.max_memory_allocated() - before == y.numel() * 2
         assert not y.requires_grad and torch.equal(y, w)
+
+
+@pytest.mark.parametrize("shape", [(0, 64), (3, 0, 64), (2, 5, 0), (0,)])
+def test_rows_with_nothing_in_them(shape):
+    # as torch's operators: results with nothing in them, gradients of the weights 0
+    td = torch.bfloat16
+    x, r = (torch.empty(shape, dtype=td, device="cuda").requires_grad_() for _ in range(2))
+    w, b = randn(shape[-1:], td, 1).requires_grad_(), randn(shape[-1:], torch.bfloat16, 2).requires_grad_()
+    d = tr.dropout(x, 0.5, 1, 2, residual=r)
+    n = tr.layer_norm(x, w, b)
+    y, h = tr.dropout_add_norm(x, r, w, b, 0.5)
+    assert all(t.shape == x.shape and t.dtype == td for t in (d, n, y, h))
+    gx, gr, gw, gb = torch.autograd.grad(d.sum() + n.sum() + y.sum() + h.sum(), (x, r, w, b))
+    assert gx.shape == gr.shape == x.shape and not gw.any() and not gb.any()
+    assert tr.LayerNorm(64)(torch.empty(0, 64, dtype=td, device="cuda")).shape == (0, 64)
+    for f in (lambda: tr.dropout(x, 1.5), lambda: tr.layer_norm(x, w, b, -1.0), lambda: tr.dropout(x.double(), 0.5), lambda: tr.layer_norm(x.double(), w.double())):
+        with pytest.raises(sdrop.SdropError):
+            f()
+
+
+def test_attention_of_nothing():
+    td = torch.float16
+    z = lambda *s: torch.ones(s, dtype=td, device="cuda").requires_grad_()      # noqa: E731
+    cu = lambda *n: torch.tensor(n, dtype=torch.int32, device="cuda")           # noqa: E731
+    # no sequences; no queries; no keys (every token's result is 0); packed, with empty sequences or none
+    cases = [((0, 5, 4, 64), (0, 7, 2, 64), {}), ((2, 0, 4, 64), (2, 7, 2, 64), {}), ((2, 5, 4, 64), (2, 0, 2, 64), {}),
+             ((2, 5, 4, 64), (2, 0, 2, 64), dict(k_len=cu(0, 0))),
+             ((0, 4, 64), (0, 2, 64), dict(cu_q=cu(0, 0, 0), cu_k=cu(0, 0, 0), max_q=0, max_k=0)), ((5, 4, 64), (0, 2, 64), dict(cu_q=cu(0, 5), cu_k=cu(0, 0), max_q=5, max_k=1)),
+             ((0, 4, 64), (6, 2, 64), dict(cu_q=cu(0, 0), cu_k=cu(0, 6), max_q=1, max_k=6)), ((3, 4, 64), (6, 2, 64), dict(cu_q=cu(0), cu_k=cu(0), max_q=1, max_k=6))]
+    for qs, ks, kw in cases:
+        for causal in (False, True):
+            q, k, v = z(*qs), z(*ks), z(*ks)
+            dirty()
+            o = tr.attention(q, k, v, causal=causal, **kw)
+            assert o.shape == q.shape and not o.any()
+            dirty()
+            for t, g in zip((q, k, v), torch.autograd.grad(o, (q, k, v), torch.ones_like(o))):
+                assert g.shape == t.shape and not g.any()
+    for shape, kw in (((0, 5, 8, 64), {}), ((2, 0, 8, 64), {}), ((0, 8, 64), dict(cu=cu(0, 0), max_len=0))):
+        x = z(*shape)
+        o = tr.qkv_attention(x, 2, causal=True, **kw)
+        g, = torch.autograd.grad(o, x, torch.ones_like(o))
+        assert o.shape == shape[:-2] + (4, 64) and g.shape == x.shape
+    for qs, ks in (((0, 5, 3, 64), (0, 7, 2, 64)), ((0, 5, 4, 60), (0, 7, 2, 60)), ((0, 5, 4, 136), (0, 7, 2, 136)), ((2, 5, 4, 64), (2, 7, 0, 64))):
+        with pytest.raises(sdrop.SdropError):
+            tr.attention(z(*qs), z(*ks), z(*ks))
+    assert sdrop.status() == 0
