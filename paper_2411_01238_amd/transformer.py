@@ -63,14 +63,22 @@ def _bound(cu, n):
     return 0 if n is None else n
 
 
-class ElementDropout(torch.nn.Module):
-    """Element-wise dropout (optionally + a residual) whose mask is never stored; a new mask every forward call in training mode."""
+def _seed(seed):
+    """A module's seed.  None: one of its own from torch's CPU generator, so that two modules, and ranks with seeds of their own, draw different
+    masks."""
+    return int(torch.randint(1 << 62, (), dtype=torch.int64, device="cpu")) if seed is None else int(seed)
 
-    def __init__(self, p=0.5, seed=0):
+
+class ElementDropout(torch.nn.Module):
+    """Element-wise dropout (optionally + a residual) whose mask is never stored; a new mask every forward call in training mode.
+    seed: None for one of the module's own (a repeated number repeats the masks).  The call's number (`calls`) is no part of the state
+    dict."""
+
+    def __init__(self, p=0.5, seed=None):
         super().__init__()
         if not 0.0 <= p <= 1.0:
             raise ValueError("p must lie in [0, 1]")
-        self.p, self.seed, self.calls = float(p), int(seed), 0
+        self.p, self.seed, self.calls = float(p), _seed(seed), 0
 
     def forward(self, x, residual=None):
         if not self.training or self.p == 0.0:
@@ -94,13 +102,13 @@ class LayerNorm(torch.nn.Module):
 
 
 class DropoutAddNorm(LayerNorm):
-    """(y, h): h = residual + dropout(x), y = norm(h).  In eval mode nothing is dropped."""
+    """(y, h): h = residual + dropout(x), y = norm(h).  In eval mode nothing is dropped.  seed: as for ElementDropout."""
 
-    def __init__(self, normalized_shape, p=0.1, eps=1e-5, bias=True, seed=0, dtype=torch.bfloat16, device="cuda"):
+    def __init__(self, normalized_shape, p=0.1, eps=1e-5, bias=True, seed=None, dtype=torch.bfloat16, device="cuda"):
         super().__init__(normalized_shape, eps, bias, dtype, device)
         if not 0.0 <= p <= 1.0:
             raise ValueError("p must lie in [0, 1]")
-        self.p, self.seed, self.calls = float(p), int(seed), 0
+        self.p, self.seed, self.calls = float(p), _seed(seed), 0
 
     def forward(self, x, residual):
         p = self.p if self.training else 0.0
