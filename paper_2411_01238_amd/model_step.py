@@ -142,19 +142,17 @@ class Block(torch.nn.Module):
         a = F.scaled_dot_product_attention(q, k, v, is_causal=self.causal)
         return self.proj(a.transpose(1, 2).reshape(B, T, d))
 
-    def step(self, x, pending=None):
-        """(x, pending): the residual stream, and what is still to be added to it: (tensor, dropout rate, seed, rng_stream) or None.
-        With ops="sdrop" that add runs in the pass of the norm that follows it, the next block's or the model's."""
+    def forward(self, x, pending=None, defer=False):
+        """x: the residual stream; pending: what is still to be added to it, (tensor, dropout rate, seed, rng_stream) or None.  Returns the
+        stream, or, with defer, (stream, pending): with ops="sdrop" that add runs in the pass of the norm that follows it, the next
+        block's or the model's."""
         p, call = (self.resid_p if self.training else 0.0), self.calls
         if self.training:
             self.calls += 1
         n, x = add_norm(self.ops, self.ln1, x, pending)
         n, x = add_norm(self.ops, self.ln2, x, (self.attend(n), p, self.seed + 4, call))
-        return x, (self.fc2(F.gelu(self.fc(n))), p, self.seed + 5, call)
-
-    def forward(self, x):
-        x, pending = self.step(x)
-        return add(self.ops, x, pending)
+        pending = (self.fc2(F.gelu(self.fc(n))), p, self.seed + 5, call)
+        return (x, pending) if defer else add(self.ops, x, pending)
 
 
 def add(ops, x, pending):
@@ -171,7 +169,7 @@ def add_norm(ops, norm, x, pending):
         return norm(x), x
     if ops == "sdrop":
         y, p, seed, rng_stream = pending
-        return _transformer().dropout_add_norm(y, x, norm.weight, norm.bias, p, norm.eps, seed, rng_stream)
+        return norm(y, x, p, seed, rng_stream)
     x = add(ops, x, pending)
     return norm(x), x
 
@@ -184,7 +182,7 @@ def run_blocks(ops, blocks, norm, x):
         return norm(x)
     pending = None
     for b in blocks:
-        x, pending = b.step(x, pending)
+        x, pending = b(x, pending, defer=True)
     return add_norm(ops, norm, x, pending)[0]
 
 

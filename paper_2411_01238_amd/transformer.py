@@ -89,7 +89,8 @@ class ElementDropout(torch.nn.Module):
 
 
 class LayerNorm(torch.nn.Module):
-    """torch.nn.LayerNorm over the last dimension, in libsdrop's kernels (its state dict loads as it is)."""
+    """torch.nn.LayerNorm over the last dimension, in libsdrop's kernels (its state dict loads as it is).  Called with a residual, it is
+    dropout_add_norm: (y, h), the dropout's numbers being the caller's."""
 
     def __init__(self, normalized_shape, eps=1e-5, bias=True, dtype=torch.bfloat16, device="cuda"):
         super().__init__()
@@ -97,8 +98,10 @@ class LayerNorm(torch.nn.Module):
         self.weight = torch.nn.Parameter(torch.ones(normalized_shape, dtype=dtype, device=device))
         self.bias = torch.nn.Parameter(torch.zeros(normalized_shape, dtype=dtype, device=device)) if bias else None
 
-    def forward(self, x):
-        return layer_norm(x, self.weight, self.bias, self.eps)
+    def forward(self, x, residual=None, p=0.0, seed=0, rng_stream=0):
+        if residual is None:
+            return layer_norm(x, self.weight, self.bias, self.eps)
+        return dropout_add_norm(x, residual, self.weight, self.bias, p, self.eps, seed, rng_stream)
 
 
 class DropoutAddNorm(LayerNorm):
@@ -112,7 +115,7 @@ class DropoutAddNorm(LayerNorm):
 
     def forward(self, x, residual):
         p = self.p if self.training else 0.0
-        out = dropout_add_norm(x, residual, self.weight, self.bias, p, self.eps, self.seed, self.calls)
+        out = super().forward(x, residual, p, self.seed, self.calls)
         if self.training:
             self.calls += 1
         return out
