@@ -64,14 +64,14 @@ def _link_native(obj):
 
 
 def build(verbose=True):
-    """Compiles every source and links libsdrop.so and the autograd module over it; always rebuilds."""
+    """Compiles every source and links libsdrop.so and the autograd module over it; always rebuilds.  The library needs no torch: it is
+    there also where the module does not build."""
     with ThreadPoolExecutor(max_workers=min(8, len(UNITS) + 1)) as ex:
         native = ex.submit(_compile_native)
         objs = list(ex.map(_compile, UNITS))
-        native = native.result()
-    cmd = [_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-Wl,-soname,libsdrop.so", "-o", LIB] + objs
-    subprocess.check_call(cmd)
-    _link_native(native)
+        cmd = [_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-Wl,-soname,libsdrop.so", "-o", LIB] + objs
+        subprocess.check_call(cmd)
+        _link_native(native.result())
     if verbose:
         print("built", LIB, "and", NATIVE)
     return LIB
