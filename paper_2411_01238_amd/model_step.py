@@ -91,6 +91,8 @@ class Linear(torch.nn.Module):
             y = ((x2 * m) @ self.weight) * (1.0 / (1.0 - p) if p < 1.0 else 0.0)
         else:
             if self.kind == "dropout_dense" and p > 0.0:
+                if self.ops == "sdrop":
+                    _transformer().refuse_recomputation()
                 x2 = _transformer().dropout(x2, p, self.seed, self.calls) if self.ops == "sdrop" else F.dropout(x2, p, training=True)
             y = x2 @ self.weight
         if self.training:
@@ -147,6 +149,8 @@ class Block(torch.nn.Module):
         stream, or, with defer, (stream, pending): with ops="sdrop" that add runs in the pass of the norm that follows it, the next
         block's or the model's."""
         p, call = (self.resid_p if self.training else 0.0), self.calls
+        if self.ops == "sdrop" and p > 0.0:
+            _transformer().refuse_recomputation()
         if self.training:
             self.calls += 1
         n, x = add_norm(self.ops, self.ln1, x, pending)

@@ -4,8 +4,9 @@ kernels; the autograd nodes around them are in csrc/autograd_native.cpp.  Each c
 results with nothing in them (attention over no keys: 0).
 
 The dropout's mask is a function of a seed and a stream number (`rng_stream`: one per call, e.g. a step counter) and is never
-stored: the backward pass draws it again.  A captured graph replays the mask of the numbers it was captured with; a module that is run
-again to save memory draws a new mask: use the functions there, with a stream number of the step's own.  Capture a backward pass only
+stored: the backward pass draws it again.  A captured graph replays the mask of the numbers it was captured with.  A module numbers its calls,
+so that one that is run again by a backward pass, to save memory, would draw another mask and is refused: use the functions there, with a
+stream number of the step's own.  Capture a backward pass only
 after the eager graphs of the same leaves are gone (torch would add their gradients on those graphs' stream, outside the capture).
 """
 import torch
@@ -69,6 +70,13 @@ def _seed(seed):
     return int(torch.randint(1 << 62, (), dtype=torch.int64, device="cpu")) if seed is None else int(seed)
 
 
+def refuse_recomputation():
+    """Raises where a backward pass is running: a call number of its own would draw another mask than the forward pass did."""
+    if torch._C._current_graph_task_id() != -1:
+        raise RuntimeError("a module that numbers its dropout masks cannot be run again in the backward pass (recomputation): it would draw another "
+                           "mask; use the functions with a seed and rng_stream of the step's own")
+
+
 class ElementDropout(torch.nn.Module):
     """Element-wise dropout (optionally + a residual) whose mask is never stored; a new mask every forward call in training mode.
     seed: None for one of the module's own (a repeated number repeats the masks).  The call's number (`calls`) is no part of the state
@@ -83,6 +91,7 @@ class ElementDropout(torch.nn.Module):
     def forward(self, x, residual=None):
         if not self.training or self.p == 0.0:
             return x if residual is None else x + residual
+        refuse_recomputation()
         y = dropout(x, self.p, self.seed, self.calls, residual)
         self.calls += 1
         return y
@@ -115,6 +124,8 @@ class DropoutAddNorm(LayerNorm):
 
     def forward(self, x, residual):
         p = self.p if self.training else 0.0
+        if p > 0.0:
+            refuse_recomputation()
         out = super().forward(x, residual, p, self.seed, self.calls)
         if self.training:
             self.calls += 1
