@@ -583,7 +583,7 @@ int sdrop_layer_norm_bwd(const void *dY, const void *dH, const void *H, const vo
  * Query head h reads key / value head h / (Hq / Hkv).  Token i of Lq sees all Lk keys of its sequence or, causal, the keys
  * j <= i + Lk - Lq (the last token sees every key: new tokens behind a cache).  A token that sees no key has O = 0, lse = -inf.
  * Products run on the matrix cores; scores, statistics and sums are fp32, P is rounded to `dtype` for the second product (what that takes from
- * keys that have a large part of their row is added).  A key
+ * keys that have a large part of their row is added, and all of it for up to 32 rows, queries x query heads of a key head).  A key
  * that a token does not see has P = 0 whatever its score; its v still takes part as 0 times v (as in the formula), so it has to
  * be finite, except behind k_len and between packed sequences, where nothing is read.
  *

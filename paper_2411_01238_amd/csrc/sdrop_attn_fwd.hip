@@ -125,7 +125,8 @@ __global__ __launch_bounds__(64 * QW * KW, QW * KW == 4 ? (HD <= 64 ? 4 : 2) : 1
                 sc[mb][e] = __builtin_amdgcn_exp2f(sc[mb][e] * P.c - mc);
                 l += sc[mb][e];
             }
-        large_from = m + fminf(__builtin_amdgcn_logf(kLargeShare * l), 8.f) * rc;
+        // (few rows wait for the memory: every tile has the product with what P's rounding took beside it)
+        if constexpr (QW > 1) large_from = m + fminf(__builtin_amdgcn_logf(kLargeShare * l), 8.f) * rc;
         const ColOperand<HD, T> va(vt);
         if constexpr (HD <= 64 && MB == 2) __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);

@@ -152,3 +152,22 @@ def test_many_keys_of_a_small_share_each(Tq, D):
     bound = e * np.abs(want) + ((np.maximum(e * p, 2.0 ** -25) + 2.0 ** -18 * p) / p.sum()) @ np.abs(vd)
     assert (np.abs(f64(o)[0, :, 0] - want) <= bound).all()
     assert (np.abs(f64(lse)[0, 0] - np.log(p.sum())) <= 2.0 ** -13).all()
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("B,Tq,Tk,Hq,Hkv,D", [(2, 1, 9000, 4, 1, 128), (1, 3, 5000, 8, 2, 64), (3, 1, 300, 2, 2, 96)])
+def test_few_queries_are_as_exact_as_their_type(B, Tq, Tk, Hq, Hkv, D, dtype):
+    # the error is that of rounding the exact result, and of values next to a tie: P's own rounding does not show
+    td = DT[dtype]
+    q, k, v = randn((B, Tq, Hq, D), td, 1), randn((B, Tk, Hkv, D), td, 2), randn((B, Tk, Hkv, D), td, 3)
+    o = f64(sdrop.sdrop_attn(q, k, v, True)[0])
+    got = want = 0.0
+    for b in range(B):
+        for h in range(Hq):
+            s = f64(q[b, :, h]) @ f64(k[b, :, h * Hkv // Hq]).T * D ** -0.5
+            s[np.arange(Tk)[None, :] > np.arange(Tq)[:, None] + Tk - Tq] = -np.inf
+            p = np.exp(s - s.max(axis=1, keepdims=True))
+            w = p / p.sum(axis=1, keepdims=True) @ f64(v[b, :, h * Hkv // Hq])
+            got += ((o[b, :, h] - w) ** 2).sum()
+            want += ((f64(torch.from_numpy(w).to(td)) - w) ** 2).sum()
+    assert got <= 1.05 ** 2 * want, np.sqrt(got / want)
