@@ -512,7 +512,7 @@ __global__ __launch_bounds__(256, HD <= 64 ? 3 : 2) void attn_dkv_kernel(AttnPar
 
 // All three gradients of sequences that one workgroup takes whole: W wavefronts own 32 keys each and walk the rows in tiles of 32, as for
 // dK and dV; their dS also goes to LDS, where the wavefronts whose turn it is multiply it with K into dQ during the next tile.  Five
-// products instead of seven, and one pass over memory (64 x 256 tokens, 8 heads of 128: 268 MB in 86 us, 3.1 TB/s; what bounds it is that the
+// products instead of seven, and one pass over memory (64 x 256 tokens, 8 heads of 128: 302 MB in 87 us, 3.5 TB/s; what bounds it is that the
 // two wavefronts of a SIMD meet at every tile, for LDS holds one workgroup per CU).
 template <class T, int HD, int W>
 __global__ __launch_bounds__(64 * W, 2) void attn_bwd_short_kernel(AttnParams P)
