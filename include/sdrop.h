@@ -628,7 +628,8 @@ int sdrop_attn(const void *q, const void *k, const void *v, void *o, void *o_res
  *     P = exp(S - lse), dP = dO v^T, dS = P (dP - row sums of dO o):   dq = scale dS k,  dk = scale dS^T q,  dv = P^T dO
  *
  * P and dS are rounded to `dtype` for their products (in fp16 times powers of two that keep them among its usual numbers, whatever the size
- * of dO), sums are fp32, dk and dv summed over the query heads that share them.  The
+ * of dO), sums are fp32, dk and dv summed over the query heads that share them.  A pair that the mask leaves out takes part as 0 times q, k, v
+ * and dO, which have to be finite (except behind k_len and between packed sequences, where nothing is read).  The
  * order of all sums is fixed: results repeat bit for bit.  dq, dk and dv are written completely (dk and dv are 0 behind k_len;
  * rows behind the last packed sequence are left as they were) and may be slices of one buffer; none may overlap an input.
  * Strides must not be 0 in an output.

@@ -809,13 +809,13 @@ bool few_rows(const AttnParams &P)
 }
 
 // One workgroup per sequence and key head, all three gradients in one pass over memory, instead of dQ and then dK and dV: up to 256 keys (what
-// LDS holds), with heads enough for a quarter of the CUs.  It walks all rows of its key head, which dQ's launch spreads over the chip: with
-// more than 256 of them, heads enough for half of the CUs, or for three quarters where heads are small and dQ is quick.  us, two launches -> one: 64 x 256 tokens, 8 heads of 128, no mask 111 -> 86, causal
-// 101 -> 76; 32 x 128, causal 32 -> 21; 8 x 256, 32 heads, 8 of keys, causal 103 -> 90; 128 x 197, 12 heads of 64 137 -> 135; 64 x 128, no
-// mask 50 -> 31; but 4 x 256, 8 heads of 128 29 -> 33.  Many rows (queries x query heads of a key head): 16 x 1024 queries over 128 keys, 32 heads of
-// 128, 8 of keys, causal 398 -> 219, 24 x 512 over 256, 64 heads of 64, 8 of keys, causal 315 -> 198; but 8 x 2048 over 256, 8 heads of 128 138 -> 200,
-// 8 x 1024 over 256, 64 heads of 128, 8 of keys 504 -> 766, 64 x 512 over 128, 32 heads of 64, 1 of keys, causal 337 -> 779, and 16 of the last
-// but 4 heads of 64 to a key head 216 -> 283.
+// LDS holds), with heads enough for a quarter of the CUs.  It walks all rows of its key head (queries x query heads of it), which dQ's launch
+// spreads over the chip: with more than 256 of them, heads enough for half of the CUs, or for three quarters where heads are small and dQ is
+// quick.  us, two launches -> one: 64 x 256 tokens, 8 heads of 128, no mask 120 -> 87, causal 106 -> 75; 32 x 128, causal 32 -> 20.5; 128 x 197,
+// 12 heads of 64 159 -> 136; 64 x 128, no mask 49 -> 31; but 4 x 256, 8 heads of 128 30 -> 33.  Many rows: 16 x 1024 queries over 128 keys,
+// 32 heads of 128, 8 of keys, causal 398 -> 219; 24 x 512 over 256, 64 heads of 64, 8 of keys, causal 315 -> 198; but 8 x 2048 over 256, 8
+// heads of 128 138 -> 200; 8 x 256, 32 heads of 128, 8 of keys, no mask 94 -> 105 (causal 95 -> 88); 8 x 1024 over 256, 64 heads of 128, 8
+// of keys 504 -> 766; 64 x 512 over 128, 32 heads of 64, 1 of keys, causal 337 -> 779.
 bool whole_sequences(const AttnParams &P)
 {
     const int64_t heads = (int64_t)P.B * P.Hkv, quarters = P.max_rows <= 256 ? 1 : P.D > 64 ? 2 : 3;
